@@ -68,8 +68,9 @@ enum {
   AKVQ_Q_PREROTATED = 8u, /* decode_attention: q arrives already rotated; skip the transform on q.
                              All four together make the library transform nothing: with inputs that were never
                              rotated this is plain round-to-nearest quantization, the ablation baseline of Table III */
-  AKVQ_OUT_FP16 = 16u     /* decode_attention: out is [B][Hq][128] binary16 (the fp32 result rounded to nearest even)
+  AKVQ_OUT_FP16 = 16u,    /* decode_attention: out is [B][Hq][128] binary16 (the fp32 result rounded to nearest even)
                              instead of fp32 */
+  AKVQ_ROPE_INVERSE = 32u /* rope_axes: turn the rows back (the transposed rotation: also the gradient of the forward one) */
 };
 
 /* Tier of a cache row written by akvq_quantize_append_tiered (Section III-C.1: text tokens 4-bit, the rest 2-bit).
@@ -280,6 +281,35 @@ int akvq_decode_step(const akvq_cache *c, const uint32_t *fine_mask, const akvq_
                      const void *v_new, const void *q, const akvq_rope *rope, int Hq, float clip, float sm_scale,
                      void *out, float *lse_out, int n_split, void *workspace, size_t workspace_bytes, uint32_t flags,
                      void *stream);
+
+/*
+ * Chunks.  The entry points below take the new rows of many sequences at once, of any lengths, packed token by token,
+ * sequence after sequence: q [n_rows][Hq][128], k and v [n_rows][Hkv][128], binary16, the heads of a row next to each other,
+ * consecutive rows q_stride, k_stride, v_stride elements apart (multiples of 8, at least the row's length), so that the three may be
+ * parts of one fused projection's output.  A chunk has at most 2^25 rows (AKVQ_ERR_UNSUPPORTED).
+ */
+
+/*
+ * akvq_rope_axes -- rotary positions on several axes (time, height and width of images and video): channel pair (i, i + 64) of
+ *   a row is turned by the angle pos[axis[i]][row] * inv_freq[i], in the pairing of akvq_rope.  A pair with inv_freq 0 stays as
+ *   it is.  pos: device, int32, any alignment of 4 bytes, n_axes rows pos_stride elements apart, one entry for every chunk row.
+ *   The angle is formed in 64 bits and its whole turns are dropped there (an error of 1e-7 at the largest position), sine and
+ *   cosine are 32-bit, the result is rounded to binary16 once.  (The fused embedding of akvq_rope reads a binary16 table instead:
+ *   akvq_rope_axes_table writes one.)  flags: AKVQ_ROPE_INVERSE or 0.
+ *   q_out / k_out may be q / k themselves with the same stride, else they may not overlap them.  Hkv = 0 (Hq = 0): no k (q).
+ *   n_rows = 0 does nothing.
+ * akvq_rope_axes_table -- the same angles as tables for akvq_rope: cos, sin [n_rows][64] binary16, 16-byte aligned.
+ */
+typedef struct akvq_axes {
+  int32_t n_axes;     /* 1 to 4 */
+  float inv_freq[64]; /* radians per position, finite */
+  uint8_t axis[64];   /* < n_axes */
+} akvq_axes;
+int akvq_rope_axes(const akvq_axes *axes, const int32_t *pos, int64_t pos_stride, int n_rows, const void *q, int64_t q_stride,
+                   int Hq, const void *k, int64_t k_stride, int Hkv, void *q_out, int64_t q_out_stride, void *k_out,
+                   int64_t k_out_stride, uint32_t flags, void *stream);
+int akvq_rope_axes_table(const akvq_axes *axes, const int32_t *pos, int64_t pos_stride, int n_rows, void *cos, void *sin,
+                         void *stream);
 
 /*
  * akvq_stream_read -- measurement aid, no part of the method: one pass of plain 128-bit loads over src (device, 16-byte

@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libakvq.so")
 
 D = 128
 MODE_TSA, MODE_PSA, MODE_PSA_SHARED = 0, 1, 2
-V_PREROTATED, OUT_ROTATED, K_PREROTATED, Q_PREROTATED, OUT_FP16 = 1, 2, 4, 8, 16
+V_PREROTATED, OUT_ROTATED, K_PREROTATED, Q_PREROTATED, OUT_FP16, ROPE_INVERSE = 1, 2, 4, 8, 16, 32
 
 EXPORTS = ["akvq_strerror", "akvq_last_hip_error", "akvq_version", "akvq_cache_bytes",
            "akvq_select_workspace_bytes", "akvq_decode_workspace_bytes", "akvq_decode_default_splits",
@@ -27,7 +27,8 @@ EXPORTS = ["akvq_strerror", "akvq_last_hip_error", "akvq_version", "akvq_cache_b
            "akvq_quantize_append_tiered", "akvq_decode_attention_tiered", "akvq_quantize_append_rope",
            "akvq_decode_attention_rope", "akvq_decode_step",
            "akvq_decode_static_scratch_bytes", "akvq_decode_attention_static",
-           "akvq_massive_workspace_bytes", "akvq_select_massive", "akvq_fold_hadamard", "akvq_stream_read"]
+           "akvq_massive_workspace_bytes", "akvq_select_massive", "akvq_fold_hadamard", "akvq_stream_read",
+           "akvq_rope_axes", "akvq_rope_axes_table"]
 TIER_2BIT, TIER_4BIT_COARSE, TIER_4BIT_FINE, TIER_PAD = 0, 1, 2, 3
 
 
@@ -41,6 +42,10 @@ class akvq_window(C.Structure):
 
 class akvq_rope(C.Structure):
     _fields_ = [("cos", C.c_void_p), ("sin", C.c_void_p), ("batch_stride", C.c_int64)]
+
+
+class akvq_axes(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("inv_freq", C.c_float * 64), ("axis", C.c_uint8 * 64)]
 
 
 class akvq_cache(C.Structure):
@@ -119,6 +124,13 @@ def lib() -> C.CDLL:
         L.akvq_decode_step.argtypes = [C.POINTER(akvq_cache), C.c_void_p, C.POINTER(akvq_window), C.c_void_p, C.c_void_p,
                                        C.c_void_p, C.POINTER(akvq_rope), C.c_int, C.c_float, C.c_float, C.c_void_p,
                                        C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_uint32, C.c_void_p]
+        L.akvq_rope_axes.restype = C.c_int
+        L.akvq_rope_axes.argtypes = [C.POINTER(akvq_axes), C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_int,
+                                     C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                     C.c_uint32, C.c_void_p]
+        L.akvq_rope_axes_table.restype = C.c_int
+        L.akvq_rope_axes_table.argtypes = [C.POINTER(akvq_axes), C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_void_p,
+                                           C.c_void_p]
         _lib = L
     return _lib
 
@@ -359,3 +371,97 @@ def decode_step(cache: Cache, k_new: torch.Tensor, v_new: torch.Tensor, q: torch
         _check(st, "akvq_decode_step")
     cache.T_len += 1
     return out, lse
+
+
+# ---- chunks: new rows of many sequences, packed token by token ------------------------------------------------------
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise AkvqError(what)
+
+
+def _on_device(*tensors) -> None:
+    """The calls go to the current device's stream: a tensor of another device (or of the host) is refused."""
+    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        _need(t is None or (t.is_cuda and t.get_device() == here), "tensors have to be on the current device")
+
+
+def _packed(t: torch.Tensor, what: str, rows: Optional[int] = None, heads: Optional[int] = None) -> int:
+    """[rows, heads, 128] fp16 whose heads lie next to each other; returns the elements from row to row."""
+    _need(t.dtype == torch.float16 and t.dim() == 3 and t.shape[2] == D, f"{what} has to be fp16 [rows, heads, 128]")
+    _need((rows is None or t.shape[0] == rows) and (heads is None or t.shape[1] == heads), f"{what}: rows or heads do not fit")
+    n, h, _ = t.shape
+    _need(t.stride(2) == 1 and (h == 1 or t.stride(1) == D), f"{what}: the heads of a row have to lie next to each other")
+    return t.stride(0) if n > 1 else h * D
+
+
+class RopeAxes:
+    """Frequencies of rotary positions with several axes: channel pair (i, i + 64) turns by pos[axis[i]] * inv_freq[i]."""
+
+    def __init__(self, inv_freq, axis):
+        inv_freq, axis = [float(f) for f in inv_freq], [int(a) for a in axis]
+        _need(len(inv_freq) == 64 and len(axis) == 64, "64 channel pairs have a frequency and an axis each")
+        _need(min(axis) >= 0 and max(axis) < 4, "axes are 0 to 3")
+        self.n_axes = max(axis) + 1
+        self._struct = akvq_axes(self.n_axes, (C.c_float * 64)(*inv_freq), (C.c_uint8 * 64)(*axis))
+
+    @classmethod
+    def sections(cls, theta: float, sections, interleaved: bool = False) -> "RopeAxes":
+        """inv_freq[i] = theta ** (-i / 64); axis a takes sections[a] pairs, one section after the other, or (interleaved) turn by
+        turn as long as its section lasts."""
+        _need(sum(sections) == 64 and min(sections) >= 0, "the sections have to be 64 pairs together")
+        if interleaved:
+            left, axis = list(sections), []
+            while len(axis) < 64:
+                for a in range(len(left)):
+                    if left[a]:
+                        axis.append(a)
+                        left[a] -= 1
+        else:
+            axis = [a for a, n in enumerate(sections) for _ in range(n)]
+        return cls([theta ** (-i / 64) for i in range(64)], axis)
+
+    def _positions(self, pos: torch.Tensor, rows: int) -> int:
+        """Checks pos ([n_axes, rows], or [rows] for one axis); returns the elements from axis to axis."""
+        _need(pos.dtype == torch.int32 and pos.dim() in (1, 2), "positions have to be int32 [axes, rows]")
+        _need(pos.shape[-1] == rows and (pos.shape[0] >= self.n_axes if pos.dim() == 2 else self.n_axes == 1),
+              "positions: one entry for every axis and row")
+        _need(rows <= 1 or pos.stride(-1) == 1, "positions: the rows of an axis have to lie next to each other")
+        return pos.stride(0) if pos.dim() == 2 and pos.shape[0] > 1 else rows
+
+
+def rope_axes(axes: RopeAxes, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None,
+              q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False):
+    """akvq_rope_axes: rotary positions of a chunk's rows, q [n, Hq, 128] and k [n, Hkv, 128] (either may be None), into q_out and k_out
+    (new tensors where None; q and k themselves turn in place).  inverse: turns back, which is also the gradient.  Returns (q_out, k_out)."""
+    _need(q is not None or k is not None, "neither q nor k")
+    rows = (q if q is not None else k).shape[0]
+    args, outs = [], []
+    for x, out, what in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            _need(out is None, f"{what}_out without {what}")
+            args += [None, 0, 0, None, 0]
+        else:
+            stride = _packed(x, what, rows)
+            if out is None:
+                out = torch.empty(x.shape, dtype=torch.float16, device=x.device)
+            args += [x.data_ptr(), stride, x.shape[1], out.data_ptr(), _packed(out, what + "_out", rows, x.shape[1])]
+        outs.append(out)
+    pos_stride = axes._positions(pos, rows)
+    _on_device(pos, q, k, *outs)
+    if rows:
+        _check(lib().akvq_rope_axes(C.byref(axes._struct), pos.data_ptr(), pos_stride, rows, *args[:3], *args[5:8], *args[3:5],
+                                    *args[8:], ROPE_INVERSE if inverse else 0, _stream()), "akvq_rope_axes")
+    return tuple(outs)
+
+
+def rope_axes_table(axes: RopeAxes, pos: torch.Tensor):
+    """akvq_rope_axes_table: (cos, sin) [rows, 64] fp16 for the calls that take rope=(cos, sin)."""
+    rows = pos.shape[-1]
+    pos_stride = axes._positions(pos, rows)
+    _on_device(pos)
+    cos, sin = (torch.empty(rows, 64, dtype=torch.float16, device=pos.device) for _ in range(2))
+    if rows:
+        _check(lib().akvq_rope_axes_table(C.byref(axes._struct), pos.data_ptr(), pos_stride, rows, cos.data_ptr(), sin.data_ptr(),
+                                          _stream()), "akvq_rope_axes_table")
+    return cos, sin

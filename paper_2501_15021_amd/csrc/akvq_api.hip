@@ -41,6 +41,8 @@ int hip_status(hipError_t e) {
 
 }  // namespace
 
+int akvq::launch_status(hipError_t e) { return hip_status(e); }
+
 extern "C" {
 
 const char *akvq_strerror(int status) {

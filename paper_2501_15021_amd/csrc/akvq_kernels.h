@@ -357,4 +357,22 @@ hipError_t launch_fold_hadamard(const uint16_t *w, uint16_t *out, int rows, int 
 // measurement aid: plain 128-bit streaming read of `bytes` bytes (a multiple of 16, at least 16)
 hipError_t launch_stream_read(const void *src, size_t bytes, uint32_t *sink, int non_temporal, hipStream_t stream);
 
+// ---- rotary positions with several axes (akvq_axes.hip) ----
+struct AxesArgs {
+  double turns[64];  // per position, of channel pair i: inv_freq[i] / 2 pi
+  uint8_t axis[64];
+  const int32_t *pos;
+  long long pos_stride;
+  int n_rows, Hq, Hkv, inverse;
+  const uint16_t *q, *k;
+  uint16_t *q_out, *k_out;  // (the tables' launch: cos, sin)
+  long long q_stride, k_stride, q_out_stride, k_out_stride;
+  int heads_per_wave;  // (set by the launcher)
+};
+hipError_t launch_rope_axes(AxesArgs a, hipStream_t stream);
+hipError_t launch_rope_axes_table(const AxesArgs &a, hipStream_t stream);
+
+// status of a launch for the C ABI; keeps a failed launch's code for akvq_last_hip_error (akvq_api.hip)
+int launch_status(hipError_t e);
+
 }  // namespace akvq
