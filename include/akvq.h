@@ -312,6 +312,47 @@ int akvq_rope_axes_table(const akvq_axes *axes, const int32_t *pos, int64_t pos_
                          void *stream);
 
 /*
+ * The cache in pages: one layer's codes and meta words in pools of n_pages pages that sequences of any lengths share.
+ *   A page holds page_rows rows (a power of two, 32 to 65536) of all KV heads:
+ *     k_codes, v_codes [n_pages][Hkv][page_rows/32][256 words], k_meta, v_meta [n_pages][Hkv][page_rows][128/G], laid out inside as in
+ *     akvq_cache.
+ *   table: device, [B][max_pages] int32: row t of sequence b is row t % page_rows of page table[b][t / page_rows].  An entry outside
+ *     [0, n_pages) names no page: rows meant for it are dropped, and its rows take no part in attention.  No page may be named twice
+ *     where rows are written.  seq_len: device, [B] int32: cached rows.  max_len: an upper bound of them that the host knows (what
+ *     lies behind it takes no part); it sizes launches and workspaces, so one bound for many steps keeps a captured call valid.
+ *   The 16-bit rows are the sequences' own, as in akvq_cache: k_sal, v_sal, sal_idx [B][Hkv][S_cap] (positions of the sequence,
+ *     ascending), sal_cnt [B][Hkv].
+ *   max_pages * page_rows must stay below 2^30.  table, seq_len and row_start need 4-byte alignment only.
+ * The new rows of a call (see "Chunks"): rows [row_start[b], row_start[b + 1]) belong to sequence b; row_start: device, [B + 1] int32,
+ *   ascending; n_rows: rows of the arrays; max_rows: an upper bound of the rows of one sequence (what exceeds it takes no part).
+ *   A sequence may have none; rows of the arrays that belong to no sequence are left alone (outputs too).
+ * Host helper akvq_paged_bytes: byte sizes of the arrays of a cache with the given shape fields (order: k_codes, v_codes, k_meta,
+ *   v_meta, k_sal, v_sal, sal_idx, sal_cnt).
+ */
+typedef struct akvq_paged {
+  int32_t B, Hkv, G, page_rows, n_pages, max_pages, S_cap, max_len;
+  uint32_t *k_codes, *v_codes; /* device */
+  uint32_t *k_meta, *v_meta;   /* device */
+  uint16_t *k_sal, *v_sal;     /* device */
+  int32_t *sal_idx, *sal_cnt;  /* device */
+  const int32_t *table, *seq_len; /* device */
+} akvq_paged;
+typedef struct akvq_chunk {
+  const int32_t *row_start; /* device */
+  int32_t n_rows, max_rows;
+} akvq_chunk;
+int akvq_paged_bytes(const akvq_paged *shape, size_t out_bytes[8]);
+
+/*
+ * akvq_paged_append -- the write path into pages: the chunk's rows of sequence b become its cache rows seq_len[b],
+ *   seq_len[b] + 1, ..., with the codes, meta words, salient bits and overlay rows that akvq_quantize_append writes for them, bit for
+ *   bit.  k, v: post-RoPE, un-rotated.  Rows behind the table's last page are dropped.  The salient lists must be final for these rows.
+ *   flags: AKVQ_K_PREROTATED, AKVQ_V_PREROTATED.  Does not modify seq_len.  n_rows = 0 does nothing.
+ */
+int akvq_paged_append(const akvq_paged *c, const akvq_chunk *rows, const void *k, int64_t k_stride, const void *v,
+                      int64_t v_stride, float clip, uint32_t flags, void *stream);
+
+/*
  * akvq_stream_read -- measurement aid, no part of the method: one pass of plain 128-bit loads over src (device, 16-byte
  *   aligned, `bytes` a multiple of 16), nothing computed but an exclusive-or, nothing stored (sink: device, one
  *   uint32, written only if the data happen to fold to a magic value).  non_temporal != 0: the loads carry the

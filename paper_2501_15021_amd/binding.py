@@ -28,7 +28,7 @@ EXPORTS = ["akvq_strerror", "akvq_last_hip_error", "akvq_version", "akvq_cache_b
            "akvq_decode_attention_rope", "akvq_decode_step",
            "akvq_decode_static_scratch_bytes", "akvq_decode_attention_static",
            "akvq_massive_workspace_bytes", "akvq_select_massive", "akvq_fold_hadamard", "akvq_stream_read",
-           "akvq_rope_axes", "akvq_rope_axes_table"]
+           "akvq_rope_axes", "akvq_rope_axes_table", "akvq_paged_bytes", "akvq_paged_append"]
 TIER_2BIT, TIER_4BIT_COARSE, TIER_4BIT_FINE, TIER_PAD = 0, 1, 2, 3
 
 
@@ -53,6 +53,18 @@ class akvq_cache(C.Structure):
                 ("S_cap", C.c_int32), ("T_len", C.c_int32),
                 ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_meta", C.c_void_p), ("v_meta", C.c_void_p),
                 ("k_sal", C.c_void_p), ("v_sal", C.c_void_p), ("sal_idx", C.c_void_p), ("sal_cnt", C.c_void_p)]
+
+
+class akvq_paged(C.Structure):
+    _fields_ = [("B", C.c_int32), ("Hkv", C.c_int32), ("G", C.c_int32), ("page_rows", C.c_int32), ("n_pages", C.c_int32),
+                ("max_pages", C.c_int32), ("S_cap", C.c_int32), ("max_len", C.c_int32),
+                ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_meta", C.c_void_p), ("v_meta", C.c_void_p),
+                ("k_sal", C.c_void_p), ("v_sal", C.c_void_p), ("sal_idx", C.c_void_p), ("sal_cnt", C.c_void_p),
+                ("table", C.c_void_p), ("seq_len", C.c_void_p)]
+
+
+class akvq_chunk(C.Structure):
+    _fields_ = [("row_start", C.c_void_p), ("n_rows", C.c_int32), ("max_rows", C.c_int32)]
 
 
 _lib = None
@@ -131,6 +143,11 @@ def lib() -> C.CDLL:
         L.akvq_rope_axes_table.restype = C.c_int
         L.akvq_rope_axes_table.argtypes = [C.POINTER(akvq_axes), C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_void_p,
                                            C.c_void_p]
+        L.akvq_paged_bytes.restype = C.c_int
+        L.akvq_paged_bytes.argtypes = [C.POINTER(akvq_paged), C.POINTER(C.c_size_t)]
+        L.akvq_paged_append.restype = C.c_int
+        L.akvq_paged_append.argtypes = [C.POINTER(akvq_paged), C.POINTER(akvq_chunk), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                        C.c_float, C.c_uint32, C.c_void_p]
         _lib = L
     return _lib
 
@@ -465,3 +482,66 @@ def rope_axes_table(axes: RopeAxes, pos: torch.Tensor):
         _check(lib().akvq_rope_axes_table(C.byref(axes._struct), pos.data_ptr(), pos_stride, rows, cos.data_ptr(), sin.data_ptr(),
                                           _stream()), "akvq_rope_axes_table")
     return cos, sin
+
+
+class PagedCache:
+    """One layer's cache in pages: pools that sequences of any lengths share, and for every sequence a row of the page table, its
+    number of cached rows and its 16-bit rows.
+
+    The caller owns the page table: it writes page numbers into table [B, max_pages] (-1: no page) and advances seq_len [B], both int32
+    on the device, so that calls can be captured and replayed while they change.  max_len is what the host knows of the longest
+    sequence (by default all that the table can name); it only sizes launches.  select_salient takes a PagedCache, too."""
+
+    def __init__(self, B: int, Hkv: int, G: int, n_pages: int, max_pages: int, page_rows: int = 64, S_cap: int = 64, device="cuda",
+                 fill: Optional[int] = None):
+        self.B, self.Hkv, self.G, self.page_rows = B, Hkv, G, page_rows
+        self.n_pages, self.max_pages, self.S_cap, self.max_len = n_pages, max_pages, S_cap, max_pages * page_rows
+        sizes = (C.c_size_t * 8)()
+        _check(lib().akvq_paged_bytes(C.byref(akvq_paged(B, Hkv, G, page_rows, n_pages, max_pages, S_cap, 0)), sizes), "akvq_paged_bytes")
+        dev = torch.device(device)
+        mk = (lambda n: torch.empty(n, dtype=torch.uint8, device=dev)) if fill is None else \
+             (lambda n: torch.full((n,), fill, dtype=torch.uint8, device=dev))
+        self.k_codes = mk(sizes[0]).view(torch.int32).view(n_pages, Hkv, page_rows // 32, 256)
+        self.v_codes = mk(sizes[1]).view(torch.int32).view(n_pages, Hkv, page_rows // 32, 256)
+        self.k_meta = mk(sizes[2]).view(torch.int32).view(n_pages, Hkv, page_rows, D // G)
+        self.v_meta = mk(sizes[3]).view(torch.int32).view(n_pages, Hkv, page_rows, D // G)
+        self.k_sal = torch.zeros(sizes[4] // 2, dtype=torch.int16, device=dev).view(B, Hkv, S_cap, D)
+        self.v_sal = torch.zeros(sizes[5] // 2, dtype=torch.int16, device=dev).view(B, Hkv, S_cap // 32, 4096)
+        self.sal_idx = torch.full((B, Hkv, S_cap), -1, dtype=torch.int32, device=dev)
+        self.sal_cnt = torch.zeros(sizes[7] // 4, dtype=torch.int32, device=dev)
+        self.table = torch.full((B, max_pages), -1, dtype=torch.int32, device=dev)
+        self.seq_len = torch.zeros(B, dtype=torch.int32, device=dev)
+        self._ws = {}
+
+    def paged_struct(self) -> akvq_paged:
+        return akvq_paged(self.B, self.Hkv, self.G, self.page_rows, self.n_pages, self.max_pages, self.S_cap, self.max_len,
+                          self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_meta.data_ptr(), self.v_meta.data_ptr(),
+                          self.k_sal.data_ptr(), self.v_sal.data_ptr(), self.sal_idx.data_ptr(), self.sal_cnt.data_ptr(),
+                          self.table.data_ptr(), self.seq_len.data_ptr())
+
+    def struct(self) -> akvq_cache:
+        """What the selection calls take: the salient lists (no code planes, which the calls for contiguous caches refuse)."""
+        return akvq_cache(self.B, self.Hkv, self.G, (self.max_pages * self.page_rows + 63) // 64 * 64, self.S_cap, 0,
+                          None, None, None, None, None, None, self.sal_idx.data_ptr(), self.sal_cnt.data_ptr())
+
+    workspace, counts, nbytes = Cache.workspace, Cache.counts, Cache.nbytes
+
+
+def _chunk(cache: PagedCache, row_start: torch.Tensor, rows: int, max_rows: int) -> akvq_chunk:
+    _need(row_start.dtype == torch.int32 and row_start.dim() == 1 and row_start.shape[0] == cache.B + 1 and row_start.is_contiguous(),
+          "row_start has to be int32 [sequences + 1]")
+    _need(max_rows >= 0, "max_rows has to be at least 0")
+    return akvq_chunk(row_start.data_ptr(), rows, max_rows)
+
+
+def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int, clip: float,
+                 flags: int = 0) -> None:
+    """akvq_paged_append: rows k, v [n, Hkv, 128] fp16 of a chunk, row_start[b] to row_start[b + 1] those of sequence b (max_rows at
+    most), become its cache rows from seq_len[b] on.  cache.seq_len is the caller's to advance."""
+    rows = k.shape[0]
+    ks, vs = _packed(k, "k", heads=cache.Hkv), _packed(v, "v", rows, cache.Hkv)
+    c, chunk = cache.paged_struct(), _chunk(cache, row_start, rows, max_rows)
+    _on_device(cache.k_codes, k, v, row_start)
+    if rows:
+        _check(lib().akvq_paged_append(C.byref(c), C.byref(chunk), k.data_ptr(), ks, v.data_ptr(), vs, clip, flags, _stream()),
+               "akvq_paged_append")

@@ -36,9 +36,72 @@ int axes_args(const akvq_axes *axes, const int32_t *pos, int64_t pos_stride, int
   return AKVQ_OK;
 }
 
+int check_paged_shape(const akvq_paged *c) {
+  if (!c || c->B <= 0 || c->Hkv <= 0 || c->page_rows <= 0 || c->n_pages <= 0 || c->max_pages <= 0 || c->S_cap <= 0 || c->max_len < 0)
+    return AKVQ_ERR_INVALID_ARG;
+  if (c->G != 64 && c->G != 128) return AKVQ_ERR_UNSUPPORTED;
+  if (c->S_cap % 64 != 0) return AKVQ_ERR_INVALID_ARG;
+  if (c->page_rows < 32 || c->page_rows > 65536 || (c->page_rows & (c->page_rows - 1)) != 0) return AKVQ_ERR_UNSUPPORTED;
+  if ((int64_t)c->max_pages * c->page_rows >= (1 << 30)) return AKVQ_ERR_UNSUPPORTED;
+  if ((int64_t)c->B * c->Hkv > 65535) return AKVQ_ERR_UNSUPPORTED;  // units index a grid dimension
+  return AKVQ_OK;
+}
+
+int paged_args(const akvq_paged *c, const akvq_chunk *rows, akvq::PagedArgs &a) {
+  const int st = check_paged_shape(c);
+  if (st != AKVQ_OK) return st;
+  const void *p[8] = {c->k_codes, c->v_codes, c->k_meta, c->v_meta, c->k_sal, c->v_sal, c->sal_idx, c->sal_cnt};
+  for (const void *x : p)
+    if (!x || !aligned(x, 16)) return AKVQ_ERR_INVALID_ARG;
+  if (!c->table || !c->seq_len || !aligned(c->table, 4) || !aligned(c->seq_len, 4)) return AKVQ_ERR_INVALID_ARG;
+  if (!rows || !rows->row_start || !aligned(rows->row_start, 4) || rows->n_rows < 0 || rows->max_rows < 0) return AKVQ_ERR_INVALID_ARG;
+  if (rows->n_rows > kMaxChunkRows) return AKVQ_ERR_UNSUPPORTED;
+  a = akvq::PagedArgs{};
+  a.k_codes = c->k_codes; a.v_codes = c->v_codes; a.k_meta = c->k_meta; a.v_meta = c->v_meta;
+  a.k_sal = c->k_sal; a.v_sal = c->v_sal; a.sal_idx = c->sal_idx; a.sal_cnt = c->sal_cnt;
+  a.table = c->table; a.seq_len = c->seq_len;
+  a.B = c->B; a.Hkv = c->Hkv; a.n_pages = c->n_pages; a.max_pages = c->max_pages; a.S_cap = c->S_cap;
+  a.page_shift = __builtin_ctz((unsigned)c->page_rows);
+  a.row_cap = c->max_pages * c->page_rows;
+  a.max_len = c->max_len < a.row_cap ? c->max_len : a.row_cap;
+  a.row_start = rows->row_start; a.n_rows = rows->n_rows;
+  a.max_rows = rows->max_rows < rows->n_rows ? rows->max_rows : rows->n_rows;
+  return AKVQ_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+int akvq_paged_bytes(const akvq_paged *shape, size_t out_bytes[8]) {
+  const int st = check_paged_shape(shape);
+  if (st != AKVQ_OK) return st;
+  if (!out_bytes) return AKVQ_ERR_INVALID_ARG;
+  const size_t rows = (size_t)shape->n_pages * shape->Hkv * shape->page_rows, units = (size_t)shape->B * shape->Hkv;
+  out_bytes[0] = out_bytes[1] = rows * 32;
+  out_bytes[2] = out_bytes[3] = rows * (128 / shape->G) * 4;
+  out_bytes[4] = out_bytes[5] = units * shape->S_cap * 256;
+  out_bytes[6] = units * shape->S_cap * 4;
+  out_bytes[7] = (units * 4 + 15) / 16 * 16;
+  return AKVQ_OK;
+}
+
+int akvq_paged_append(const akvq_paged *c, const akvq_chunk *rows, const void *k, int64_t k_stride, const void *v,
+                      int64_t v_stride, float clip, uint32_t flags, void *stream) {
+  akvq::PagedAppendArgs a{};
+  const int st = paged_args(c, rows, a.c);
+  if (st != AKVQ_OK) return st;
+  if (!(clip > 0.0f) || clip > 1.0f) return AKVQ_ERR_INVALID_ARG;
+  if (flags & ~(uint32_t)(AKVQ_K_PREROTATED | AKVQ_V_PREROTATED)) return AKVQ_ERR_INVALID_ARG;
+  if (a.c.max_rows == 0) return AKVQ_OK;
+  if (check_rows(k, k_stride, c->Hkv) != AKVQ_OK || check_rows(v, v_stride, c->Hkv) != AKVQ_OK) return AKVQ_ERR_INVALID_ARG;
+  a.k = static_cast<const uint16_t *>(k); a.v = static_cast<const uint16_t *>(v);
+  a.k_stride = k_stride; a.v_stride = v_stride;
+  a.clip = clip;
+  a.rotate_k = (flags & AKVQ_K_PREROTATED) ? 0 : 1;
+  a.rotate_v = (flags & AKVQ_V_PREROTATED) ? 0 : 1;
+  return akvq::launch_status(akvq::launch_paged_append(a, c->G, static_cast<hipStream_t>(stream)));
+}
 
 int akvq_rope_axes(const akvq_axes *axes, const int32_t *pos, int64_t pos_stride, int n_rows, const void *q, int64_t q_stride,
                    int Hq, const void *k, int64_t k_stride, int Hkv, void *q_out, int64_t q_out_stride, void *k_out,

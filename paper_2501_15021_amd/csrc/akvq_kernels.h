@@ -372,6 +372,38 @@ struct AxesArgs {
 hipError_t launch_rope_axes(AxesArgs a, hipStream_t stream);
 hipError_t launch_rope_axes_table(const AxesArgs &a, hipStream_t stream);
 
+// ---- the cache in pages (akvq_paged_append.hip, akvq_paged_attention.hip) ----
+// Pools and sequences of akvq_paged; row t of sequence b lies in page table[b][t >> page_shift].
+struct PagedArgs {
+  uint32_t *k_codes, *v_codes, *k_meta, *v_meta;
+  uint16_t *k_sal, *v_sal;
+  const int32_t *sal_idx, *sal_cnt, *table, *seq_len;
+  int B, Hkv, page_shift, n_pages, max_pages, S_cap, max_len;
+  int row_cap;  // rows a sequence's table can name
+  // the chunk: rows [row_start[b], row_start[b + 1]) of n_rows are sequence b's, max_rows of them at most
+  const int32_t *row_start;
+  int n_rows, max_rows;
+};
+// The cached length of a sequence and its share of the chunk, as the kernels take them: what the device arrays hold is brought
+// into range, whatever it is.
+struct ChunkSpan { int len, first, rows; };
+__host__ __device__ inline ChunkSpan chunk_span(int len, int first, int end, const PagedArgs &a) {
+  ChunkSpan s;
+  s.len = len < 0 ? 0 : len > a.max_len ? a.max_len : len;
+  s.first = first < 0 ? 0 : first > a.n_rows ? a.n_rows : first;
+  end = end < s.first ? s.first : end > a.n_rows ? a.n_rows : end;
+  s.rows = end - s.first < a.max_rows ? end - s.first : a.max_rows;
+  return s;
+}
+struct PagedAppendArgs {
+  PagedArgs c;
+  const uint16_t *k, *v;
+  long long k_stride, v_stride;
+  float clip;
+  int rotate_k, rotate_v;
+};
+hipError_t launch_paged_append(const PagedAppendArgs &a, int G, hipStream_t stream);
+
 // status of a launch for the C ABI; keeps a failed launch's code for akvq_last_hip_error (akvq_api.hip)
 int launch_status(hipError_t e);
 

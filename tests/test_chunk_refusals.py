@@ -66,3 +66,62 @@ def test_binding_of_rope_axes():
             (pos, x, None, {}, "current device")]:
         with pytest.raises(akvq.AkvqError, match=why):
             akvq.rope_axes(axes, p, q, k, **kw)
+
+
+def _paged(**kw):
+    f = dict(B=2, Hkv=4, G=128, page_rows=64, n_pages=5, max_pages=3, S_cap=64, max_len=100)
+    p = {n: P for n in ("k_codes", "v_codes", "k_meta", "v_meta", "k_sal", "v_sal", "sal_idx", "sal_cnt", "table", "seq_len")}
+    for d in (f, p):
+        d.update({n: v for n, v in kw.items() if n in d})
+    return akvq.akvq_paged(*f.values(), *p.values())
+
+
+SHAPES = [
+    (dict(B=0), INVALID), (dict(Hkv=0), INVALID), (dict(G=32), UNSUPPORTED), (dict(page_rows=0), INVALID), (dict(page_rows=16), UNSUPPORTED),
+    (dict(page_rows=96), UNSUPPORTED), (dict(page_rows=1 << 17), UNSUPPORTED), (dict(n_pages=0), INVALID), (dict(max_pages=0), INVALID),
+    (dict(S_cap=0), INVALID), (dict(S_cap=96), INVALID), (dict(max_len=-1), INVALID), (dict(max_pages=1 << 24), UNSUPPORTED),
+    (dict(B=20000), UNSUPPORTED)]
+POINTERS = [(dict([(n, x)]), INVALID) for n in ("k_codes", "v_codes", "k_meta", "v_meta", "k_sal", "v_sal", "sal_idx", "sal_cnt") for x in (None, ODD)]
+POINTERS += [(dict([(n, x)]), INVALID) for n in ("table", "seq_len") for x in (None, C.c_void_p((1 << 20) + 2))]
+CHUNKS = [((None, 5, 5), INVALID), ((C.c_void_p((1 << 20) + 1), 5, 5), INVALID), ((P, -1, 5), INVALID), ((P, 5, -1), INVALID),
+          ((P, (1 << 25) + 1, 5), UNSUPPORTED), ((P, 0, 5), OK), ((P, 5, 0), OK)]
+
+
+def test_paged_bytes():
+    sizes = (C.c_size_t * 8)()
+    assert akvq.lib().akvq_paged_bytes(C.byref(_paged()), sizes) == OK
+    assert list(sizes) == [5 * 4 * 64 * 32] * 2 + [5 * 4 * 64 * 4] * 2 + [8 * 64 * 256] * 2 + [8 * 64 * 4, 32]
+    assert akvq.lib().akvq_paged_bytes(C.byref(_paged(G=64)), sizes) == OK and sizes[2] == 5 * 4 * 64 * 8
+    assert akvq.lib().akvq_paged_bytes(C.byref(_paged()), None) == INVALID
+    for kw, want in SHAPES:
+        assert akvq.lib().akvq_paged_bytes(C.byref(_paged(**kw)), sizes) == want, kw
+
+
+def test_paged_append():
+    def call(c=None, rows=(P, 5, 5), k=P, ks=512, v=P, vs=512, clip=0.8, flags=0):
+        return akvq.lib().akvq_paged_append(C.byref(c or _paged()), C.byref(akvq.akvq_chunk(*rows)), k, ks, v, vs, clip, flags, None)
+    for kw, want in SHAPES + POINTERS:
+        assert call(_paged(**kw)) == want, kw
+    for rows, want in CHUNKS:
+        assert call(rows=rows) == want, rows
+    for kw in (dict(k=None), dict(k=ODD), dict(ks=504), dict(ks=516), dict(v=None), dict(v=ODD), dict(vs=0), dict(clip=0.0), dict(clip=1.5),
+               dict(clip=float("nan")), dict(flags=2), dict(flags=16), dict(flags=32)):
+        assert call(**kw) == INVALID, kw
+    assert akvq.lib().akvq_paged_append(C.byref(_paged()), None, P, 512, P, 512, 0.8, 0, None) == INVALID
+    assert akvq.lib().akvq_paged_append(None, C.byref(akvq.akvq_chunk(P, 5, 5)), P, 512, P, 512, 0.8, 0, None) == INVALID
+
+
+def test_binding_of_paged_append():
+    c = akvq.PagedCache(2, 4, 128, 5, 3, device="cpu", fill=0)
+    assert c.k_codes.shape == (5, 4, 2, 256) and c.v_meta.shape == (5, 4, 64, 1) and c.max_len == 192 and bool((c.table == -1).all())
+    x, start = torch.zeros(5, 4, 128, dtype=torch.float16), torch.tensor([0, 2, 5], dtype=torch.int32)
+    for k, v, s, m, why in [(x.float(), x, start, 3, "fp16"), (x[:, :3], x[:, :3], start, 3, "do not fit"), (x, x[:4], start, 3, "do not fit"),
+                            (x, x, start[:2], 3, "row_start"), (x, x, start.long(), 3, "row_start"), (x, x, start, -1, "max_rows"),
+                            (x, x, start, 3, "current device")]:
+        with pytest.raises(akvq.AkvqError, match=why):
+            akvq.paged_append(c, k, v, s, m, 0.8)
+    with pytest.raises(akvq.AkvqError):
+        akvq.PagedCache(2, 4, 128, 5, 3, page_rows=48, device="cpu")
+    # a call for contiguous caches takes no pages
+    s = c.struct()
+    assert akvq.lib().akvq_quantize_append(C.byref(s), P, P, 1, 0.8, 0, None) == INVALID
