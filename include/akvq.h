@@ -353,6 +353,27 @@ int akvq_paged_append(const akvq_paged *c, const akvq_chunk *rows, const void *k
                       int64_t v_stride, float clip, uint32_t flags, void *stream);
 
 /*
+ * akvq_paged_attention -- attention of a chunk's rows over the cached rows of their sequences and over the chunk itself:
+ *   out[i][hq] = softmax_j( sm_scale * s_ij ) v_j over the rows j < seq_len[b] of the pages (as akvq_decode_attention reads them) and the
+ *   chunk's rows j <= i of the same sequence, which count as they arrive (binary16), whether or not akvq_paged_append has already
+ *   stored them behind seq_len.  One row a sequence is the decode step of a batch of unequal lengths; nothing cached is a first chunk.
+ *   q, k, v: post-RoPE, un-rotated.  out: [n_rows][Hq][128] binary16, rows out_stride elements apart.  lse_out: optional, [n_rows][Hq]
+ *   fp32.  Hq / Hkv at most 8.  fp32 scores, sums and accumulators; the cached rows' queries as integers of 20 bits (16 against
+ *   16-bit rows), weights of 11 bits (16 for the 16-bit rows).
+ *   Rows listed as salient are read from the overlay whatever their page.  NaN or infinity in a sequence's own rows gives
+ *   unspecified values for that sequence and KV head, never for others.
+ *   flags: AKVQ_Q_PREROTATED (q and k arrive rotated), AKVQ_OUT_ROTATED (the chunk's v rows arrive rotated, out is left rotated).
+ *   n_split <= 0 lets the library choose, akvq_paged_default_splits() at most; larger than 1024 is refused.  workspace: device,
+ *   akvq_paged_workspace_bytes() bytes of n_split, or of that maximum (0 bytes, and NULL, for one split); calls that may overlap need
+ *   one each.  out may not overlap q, k or v.  n_rows = 0 does nothing.
+ */
+size_t akvq_paged_workspace_bytes(int n_rows, int Hq, int n_split);
+int akvq_paged_default_splits(const akvq_paged *c, int Hq, int max_rows);
+int akvq_paged_attention(const akvq_paged *c, const akvq_chunk *rows, const void *q, int64_t q_stride, int Hq, const void *k,
+                         int64_t k_stride, const void *v, int64_t v_stride, float sm_scale, void *out, int64_t out_stride,
+                         float *lse_out, int n_split, void *workspace, size_t workspace_bytes, uint32_t flags, void *stream);
+
+/*
  * akvq_stream_read -- measurement aid, no part of the method: one pass of plain 128-bit loads over src (device, 16-byte
  *   aligned, `bytes` a multiple of 16), nothing computed but an exclusive-or, nothing stored (sink: device, one
  *   uint32, written only if the data happen to fold to a magic value).  non_temporal != 0: the loads carry the

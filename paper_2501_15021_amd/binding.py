@@ -28,7 +28,8 @@ EXPORTS = ["akvq_strerror", "akvq_last_hip_error", "akvq_version", "akvq_cache_b
            "akvq_decode_attention_rope", "akvq_decode_step",
            "akvq_decode_static_scratch_bytes", "akvq_decode_attention_static",
            "akvq_massive_workspace_bytes", "akvq_select_massive", "akvq_fold_hadamard", "akvq_stream_read",
-           "akvq_rope_axes", "akvq_rope_axes_table", "akvq_paged_bytes", "akvq_paged_append"]
+           "akvq_rope_axes", "akvq_rope_axes_table", "akvq_paged_bytes", "akvq_paged_append",
+           "akvq_paged_workspace_bytes", "akvq_paged_default_splits", "akvq_paged_attention"]
 TIER_2BIT, TIER_4BIT_COARSE, TIER_4BIT_FINE, TIER_PAD = 0, 1, 2, 3
 
 
@@ -148,6 +149,14 @@ def lib() -> C.CDLL:
         L.akvq_paged_append.restype = C.c_int
         L.akvq_paged_append.argtypes = [C.POINTER(akvq_paged), C.POINTER(akvq_chunk), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                         C.c_float, C.c_uint32, C.c_void_p]
+        L.akvq_paged_workspace_bytes.restype = C.c_size_t
+        L.akvq_paged_workspace_bytes.argtypes = [C.c_int] * 3
+        L.akvq_paged_default_splits.restype = C.c_int
+        L.akvq_paged_default_splits.argtypes = [C.POINTER(akvq_paged), C.c_int, C.c_int]
+        L.akvq_paged_attention.restype = C.c_int
+        L.akvq_paged_attention.argtypes = [C.POINTER(akvq_paged), C.POINTER(akvq_chunk), C.c_void_p, C.c_int64, C.c_int, C.c_void_p,
+                                           C.c_int64, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_int,
+                                           C.c_void_p, C.c_size_t, C.c_uint32, C.c_void_p]
         _lib = L
     return _lib
 
@@ -545,3 +554,30 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, row_start:
     if rows:
         _check(lib().akvq_paged_append(C.byref(c), C.byref(chunk), k.data_ptr(), ks, v.data_ptr(), vs, clip, flags, _stream()),
                "akvq_paged_append")
+
+
+def paged_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int,
+                    sm_scale: float, n_split: int = 0, flags: int = 0, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """akvq_paged_attention: a chunk's rows q [n, Hq, 128], k and v [n, Hkv, 128] fp16 (row_start and max_rows as in paged_append) over the
+    cached rows of their sequences and over the chunk's own rows up to each.  Returns out [n, Hq, 128] fp16; lse [n, Hq] fp32 is
+    written where given.  Rows that belong to no sequence are left as they are."""
+    rows, Hq = q.shape[0], q.shape[1] if q.dim() == 3 else 0
+    qs, ks, vs = _packed(q, "q"), _packed(k, "k", rows, cache.Hkv), _packed(v, "v", rows, cache.Hkv)
+    c, chunk = cache.paged_struct(), _chunk(cache, row_start, rows, max_rows)
+    if out is None:
+        out = torch.empty(rows, Hq, D, dtype=torch.float16, device=q.device)
+    os_ = _packed(out, "out", rows, Hq)
+    _need(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (rows, Hq)),
+          "lse has to be fp32 [rows, Hq]")
+    _on_device(cache.k_codes, q, k, v, row_start, out, lse)
+    if rows:
+        L = lib()
+        if n_split <= 0:
+            n_split = L.akvq_paged_default_splits(C.byref(c), Hq, min(max_rows, rows))
+        nws = L.akvq_paged_workspace_bytes(rows, Hq, n_split)
+        # of its own for every call: calls on two streams, or two captured graphs, share none
+        ws = torch.empty(nws, dtype=torch.uint8, device=q.device) if nws else None
+        _check(L.akvq_paged_attention(C.byref(c), C.byref(chunk), q.data_ptr(), qs, Hq, k.data_ptr(), ks, v.data_ptr(), vs, sm_scale,
+                                      out.data_ptr(), os_, _ptr(lse), n_split, _ptr(ws), nws, flags, _stream()), "akvq_paged_attention")
+    return out

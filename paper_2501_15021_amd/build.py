@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libakvq.so")
 NOWAIT = os.path.join(HERE, "libakvq_nowait.so")
 SOURCES = ["akvq_api.hip", "akvq_quantize.hip", "akvq_decode.hip", "akvq_select.hip", "akvq_fold.hip", "akvq_stream.hip",
-           "akvq_chunk_api.hip", "akvq_axes.hip", "akvq_paged_append.hip"]
+           "akvq_chunk_api.hip", "akvq_axes.hip", "akvq_paged_append.hip", "akvq_paged_attention.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

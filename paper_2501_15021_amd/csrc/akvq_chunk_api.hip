@@ -139,4 +139,44 @@ int akvq_rope_axes_table(const akvq_axes *axes, const int32_t *pos, int64_t pos_
   return akvq::launch_status(akvq::launch_rope_axes_table(a, static_cast<hipStream_t>(stream)));
 }
 
+size_t akvq_paged_workspace_bytes(int n_rows, int Hq, int n_split) {
+  if (n_rows <= 0 || Hq <= 0 || n_split <= 1) return 0;
+  return (size_t)n_rows * Hq * n_split * akvq::kPartialStride * sizeof(float);
+}
+
+int akvq_paged_default_splits(const akvq_paged *c, int Hq, int max_rows) {
+  if (check_paged_shape(c) != AKVQ_OK || Hq <= 0 || Hq % c->Hkv != 0 || max_rows <= 0) return 1;
+  const int64_t cap = (int64_t)c->max_pages * c->page_rows;
+  return akvq::paged_splits((long)c->B * c->Hkv, (long)max_rows * (Hq / c->Hkv), (long)(c->max_len < cap ? c->max_len : cap));
+}
+
+int akvq_paged_attention(const akvq_paged *c, const akvq_chunk *rows, const void *q, int64_t q_stride, int Hq, const void *k,
+                         int64_t k_stride, const void *v, int64_t v_stride, float sm_scale, void *out, int64_t out_stride,
+                         float *lse_out, int n_split, void *workspace, size_t workspace_bytes, uint32_t flags, void *stream) {
+  akvq::PagedAttentionArgs a{};
+  const int st = paged_args(c, rows, a.c);
+  if (st != AKVQ_OK) return st;
+  if (Hq <= 0 || Hq % c->Hkv != 0) return AKVQ_ERR_INVALID_ARG;
+  if (Hq / c->Hkv > 8) return AKVQ_ERR_UNSUPPORTED;
+  if ((int64_t)rows->n_rows * Hq >= (1ll << 31)) return AKVQ_ERR_UNSUPPORTED;
+  if (flags & ~(uint32_t)(AKVQ_Q_PREROTATED | AKVQ_OUT_ROTATED) || n_split > 1024) return AKVQ_ERR_INVALID_ARG;
+  if (a.c.max_rows == 0) return AKVQ_OK;
+  if (check_rows(q, q_stride, Hq) != AKVQ_OK || check_rows(k, k_stride, c->Hkv) != AKVQ_OK || check_rows(v, v_stride, c->Hkv) != AKVQ_OK ||
+      check_rows(out, out_stride, Hq) != AKVQ_OK)
+    return AKVQ_ERR_INVALID_ARG;
+  if (lse_out && !aligned(lse_out, 4)) return AKVQ_ERR_INVALID_ARG;
+  if (n_split <= 0) n_split = akvq_paged_default_splits(c, Hq, a.c.max_rows);
+  if (n_split > 1) {
+    if (!workspace || !aligned(workspace, 16)) return AKVQ_ERR_INVALID_ARG;
+    if (workspace_bytes < akvq_paged_workspace_bytes(rows->n_rows, Hq, n_split)) return AKVQ_ERR_WORKSPACE;
+  }
+  a.q = static_cast<const uint16_t *>(q); a.k = static_cast<const uint16_t *>(k); a.v = static_cast<const uint16_t *>(v);
+  a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.out_stride = out_stride;
+  a.out = static_cast<uint16_t *>(out); a.lse = lse_out; a.partial = static_cast<float *>(workspace);
+  a.Hq = Hq; a.n_split = n_split; a.sm_scale = sm_scale;
+  a.q_rotated = (flags & AKVQ_Q_PREROTATED) ? 1 : 0;
+  a.out_rotated = (flags & AKVQ_OUT_ROTATED) ? 1 : 0;
+  return akvq::launch_status(akvq::launch_paged_attention(a, c->G, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

@@ -404,6 +404,28 @@ struct PagedAppendArgs {
 };
 hipError_t launch_paged_append(const PagedAppendArgs &a, int G, hipStream_t stream);
 
+struct PagedAttentionArgs {
+  PagedArgs c;
+  const uint16_t *q, *k, *v;
+  long long q_stride, k_stride, v_stride, out_stride;
+  uint16_t *out;   // [n_rows][Hq][128] binary16
+  float *lse;      // optional [n_rows][Hq]
+  float *partial;  // [n_rows][Hq][n_split][kPartialStride]
+  int Hq, n_split;
+  float sm_scale;
+  int q_rotated, out_rotated;
+};
+hipError_t launch_paged_attention(const PagedAttentionArgs &a, int G, hipStream_t stream);
+// How many splits of the keys, for units (sequences x KV heads) of at most `rows` rows (tokens x heads of a group) over at most `len`
+// cached rows: so many that two workgroups a CU find work, with eight blocks of 32 keys for each of them.
+inline int paged_splits(long units, long rows, long len) {
+  const long blocks = (len + 31) / 32, tiles = rows <= 16 ? 1 : rows <= 64 ? (rows + 31) / 32 : (rows + 127) / 128;
+  long want = 512 / (units * tiles);
+  if (want > blocks / 8) want = blocks / 8;
+  if (want > 32) want = 32;
+  return (int)(want < 1 ? 1 : want);
+}
+
 // status of a launch for the C ABI; keeps a failed launch's code for akvq_last_hip_error (akvq_api.hip)
 int launch_status(hipError_t e);
 

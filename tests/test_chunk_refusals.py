@@ -125,3 +125,40 @@ def test_binding_of_paged_append():
     # a call for contiguous caches takes no pages
     s = c.struct()
     assert akvq.lib().akvq_quantize_append(C.byref(s), P, P, 1, 0.8, 0, None) == INVALID
+
+
+def test_paged_attention():
+    def call(c=None, rows=(P, 5, 5), q=P, qs=1024, Hq=8, k=P, ks=512, v=P, vs=512, out=P, os=1024, lse=None, n_split=1, ws=None, nws=0, flags=0):
+        return akvq.lib().akvq_paged_attention(C.byref(c or _paged()), C.byref(akvq.akvq_chunk(*rows)), q, qs, Hq, k, ks, v, vs, 0.1, out, os, lse,
+                                               n_split, ws, nws, flags, None)
+    for kw, want in SHAPES + POINTERS:
+        assert call(_paged(**kw)) == want, kw
+    for rows, want in CHUNKS:
+        assert call(rows=rows) == want, rows
+    for kw in (dict(q=None), dict(q=ODD), dict(qs=1016), dict(qs=1028), dict(Hq=0), dict(Hq=6), dict(k=None), dict(k=ODD), dict(ks=504), dict(v=None),
+               dict(v=ODD), dict(vs=504), dict(out=None), dict(out=ODD), dict(os=1016), dict(lse=C.c_void_p((1 << 20) + 2)), dict(n_split=1025),
+               dict(flags=1), dict(flags=4), dict(flags=16), dict(n_split=2), dict(n_split=2, ws=ODD, nws=1 << 30)):
+        assert call(**kw) == INVALID, kw
+    assert call(Hq=36, qs=36 * 128, os=36 * 128) == UNSUPPORTED
+    need = akvq.lib().akvq_paged_workspace_bytes(5, 8, 2)
+    assert need == 5 * 8 * 2 * 132 * 4 and akvq.lib().akvq_paged_workspace_bytes(5, 8, 1) == 0 == akvq.lib().akvq_paged_workspace_bytes(0, 8, 2)
+    assert call(n_split=2, ws=P, nws=need - 1) == -4
+
+
+def test_default_splits():
+    L = akvq.lib()
+    for B, Hkv, Hq, rows, length in ((1, 32, 32, 1, 640), (16, 32, 32, 1, 4096), (32, 4, 28, 1, 32768), (4, 8, 32, 8, 8191), (1, 1, 8, 4096, 1 << 20), (2, 2, 2, 1, 0)):
+        c = _paged(B=B, Hkv=Hkv, max_pages=1 << 15, max_len=length)
+        n = L.akvq_paged_default_splits(C.byref(c), Hq, rows)
+        assert 1 <= n <= 32 and n <= max(1, length // 32)
+    assert L.akvq_paged_default_splits(C.byref(_paged()), 6, 1) == 1 and L.akvq_paged_default_splits(None, 6, 1) == 1
+
+
+def test_binding_of_paged_attention():
+    c = akvq.PagedCache(2, 4, 128, 5, 3, device="cpu", fill=0)
+    q, x, start = torch.zeros(5, 8, 128, dtype=torch.float16), torch.zeros(5, 4, 128, dtype=torch.float16), torch.tensor([0, 2, 5], dtype=torch.int32)
+    for q_, k, v, kw, why in [(q.float(), x, x, {}, "fp16"), (q, x[:4], x, {}, "do not fit"), (q, x, x[:, :2], {}, "do not fit"),
+                              (q, x, x, dict(out=q[:4]), "do not fit"), (q, x, x, dict(lse=torch.zeros(5, 4)), "lse"), (q[:, 0], x, x, {}, "fp16"),
+                              (q, x, x, {}, "current device")]:
+        with pytest.raises(akvq.AkvqError, match=why):
+            akvq.paged_attention(c, q_, k, v, start, 3, 0.1, **kw)
