@@ -24,8 +24,9 @@
 namespace akvq {
 namespace {
 
-constexpr int kDigits = 4;
-constexpr int kPagedWaves = 4;
+constexpr int kDigits = 4;  // 3 or 4
+constexpr int kFewWaves = 4;   // of a workgroup that has few rows: they share them and deal the keys among them
+constexpr int kManyWaves = 8;  // of a workgroup that has many: each has its own, and all look at the same keys
 constexpr float kNoScore = -1.0e30f;   // reference before the first score
 constexpr float kRaiseAt = 15.0f;      // a score may exceed the reference by this (2^15 is the largest weight) ...
 constexpr float kRaiseTo = 7.0f;       // ... and then gets a reference this far below it
@@ -51,12 +52,13 @@ __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
   asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
   return r;
 }
-// rows: codes as 4-bit floats; columns: query digits as 6-bit floats, times 2^(scale - 127)
+// rows: codes as 4-bit floats; columns: query digits as 6-bit floats, times 2^(byte DIGIT of scale - 127)
+template <int DIGIT>
 __device__ __forceinline__ f32x4 mfma_codes(u32x4 codes, u32x6 digits, uint32_t scale, f32x4 c) {
   constexpr int kE2M3 = 2, kE2M1 = 4;
   const i32x8 a = {(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3], 0, 0, 0, 0};
   const i32x8 b = {(int)digits[0], (int)digits[1], (int)digits[2], (int)digits[3], (int)digits[4], (int)digits[5], 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, kE2M1, kE2M3, 0, 127, 0, (int)scale);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, kE2M1, kE2M3, 0, 127, DIGIT, (int)scale);
 }
 __device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -132,6 +134,7 @@ struct BlockMeta {
   float v_rcp[32];                        // 4^ii / that scale (no part: 0)
   float v_share[NG][32];                  // scale / that scale (two groups only)
   uint16_t v_zero[2][NG][32];             // binary16, in the weights' order: zero-point * 4^(ii - 3), low part and multiples of 2048
+  uint16_t none[32];                      // zeros (two groups only)
 };
 
 template <int NG>
@@ -141,26 +144,39 @@ struct CodeBlock {
   int limit;          // rows from here on (of the sequence) take no part
 };
 
-// WK of the four wavefronts of a workgroup share its rows and deal the keys among them; the others have rows of their own.
-template <int G, int QT, int WK>
-struct PagedShared {
-  static constexpr int NG = kD / G;
-  static constexpr int kRows = 16 * QT;      // of a wavefront
-  static constexpr int kVStride = kD + 16;   // binary16 values: the rows of a transposing read fall on different banks
-  BlockMeta<NG> meta[kPagedWaves];
-  __attribute__((aligned(16))) uint16_t v[kPagedWaves][32][kVStride];
-  float o[WK > 1 ? WK : 1][WK > 1 ? kRows : 1][WK > 1 ? kD + 4 : 1];
-  float m[WK][kRows], l[WK][kRows];
+__device__ __forceinline__ void lds_barrier() {  // leaves loads from memory in flight
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Rows of 16 chunks of 16 bytes in LDS: chunk c of row r lies at place c ^ 2 (r % 8), so that eight rows' chunks of the same number fall
+// on all banks, read whole (a key operand) or as the two chunks of a transposing read.
+__device__ __forceinline__ int staged_at(int row, int chunk) { return row * kD + ((chunk ^ (2 * (row & 7))) << 3); }
+constexpr int kStage = 64;  // rows of 16-bit keys and values that a workgroup of many rows holds in LDS at a time (two such stages)
+
+template <int G, int QT, bool MANY>
+struct PagedShared;
+template <int G, int QT>
+struct PagedShared<G, QT, true> {
+  BlockMeta<kD / G> meta[kManyWaves];
+  __attribute__((aligned(16))) uint16_t k[2][kStage * kD], v[2][kStage * kD];
+};
+template <int G, int QT>
+struct PagedShared<G, QT, false> {
+  BlockMeta<kD / G> meta[kFewWaves];
+  __attribute__((aligned(16))) uint16_t v[kFewWaves][32 * kD];
+  __attribute__((aligned(16))) float o[kFewWaves][16 * QT][kD + 4];
+  float m[kFewWaves][16 * QT], l[kFewWaves][16 * QT];
 };
 
-template <int G, int QT, int WK>
-__global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(PagedAttentionArgs a) {
-  constexpr int NG = kD / G, WR = kPagedWaves / WK, kRows = 16 * QT;
-  using Shared = PagedShared<G, QT, WK>;
-  __shared__ Shared sh;
+template <int G, int QT, bool MANY>
+__global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged_attention_kernel(PagedAttentionArgs a) {
+  constexpr int NG = kD / G, NW = MANY ? kManyWaves : kFewWaves, WR = MANY ? NW : 1, WK = NW / WR, kRows = 16 * QT;
+  __shared__ PagedShared<G, QT, MANY> sh;
   const PagedArgs &c = a.c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-  const int wk = WK > 1 ? wave : 0, wr = WK > 1 ? 0 : wave;
+  const int wk = MANY ? 0 : wave, wr = MANY ? wave : 0;
   const int unit = blockIdx.y, b = unit / c.Hkv, head = unit % c.Hkv, R = a.Hq / c.Hkv, split = blockIdx.z;
   const ChunkSpan s = chunk_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
   const int rows = s.rows * R;                                  // of this unit: token by token, the heads of the group
@@ -191,7 +207,7 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(Paged
 
   f32x4 o[QT][8];
   float m[QT], l[QT];
-  u32x4 raw[QT][4];  // the queries as they arrive: lane (n, q) holds channels 32m + 8q .. + 7 of its column's row
+  const uint16_t *q_at[QT];  // of this lane's column
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
 #pragma unroll
@@ -199,18 +215,24 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(Paged
     m[t] = kNoScore;
     l[t] = 0.0f;
     const int row = min(row0 + 16 * t + n, rows - 1), token = row / R;
-    const uint16_t *p = a.q + (s.first + token) * a.q_stride + (head * R + row - token * R) * kD + 8 * q;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) raw[t][k] = *reinterpret_cast<const u32x4 *>(p + 32 * k);
+    q_at[t] = a.q + (s.first + token) * a.q_stride + (head * R + row - token * R) * kD + 8 * q;
   }
+  // the query as it arrives: lane (n, q) holds channels 32m + 8q .. + 7 of its column's row (read again by each kind of keys: kept, it
+  // would take 32 registers all along)
+  auto load_query = [&](int t, u32x4 (&raw)[4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) raw[k] = *reinterpret_cast<const u32x4 *>(q_at[t] + 32 * k);
+  };
   // the rotated query, times sm_scale * log2(e): products with it are base-2 logits
   auto rotated = [&](int t, float (&x)[32]) {
+    u32x4 raw[4];
+    load_query(t, raw);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        x[8 * k + 2 * w] = half_bits_to_float(raw[t][k][w] & 0xFFFFu);
-        x[8 * k + 2 * w + 1] = half_bits_to_float(raw[t][k][w] >> 16);
+        x[8 * k + 2 * w] = half_bits_to_float(raw[k][w] & 0xFFFFu);
+        x[8 * k + 2 * w + 1] = half_bits_to_float(raw[k][w] >> 16);
       }
     float f = sm2;
     if (!a.q_rotated) {
@@ -262,58 +284,69 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(Paged
       const uint32_t e_biased = min(max(__float_as_uint(mx) >> 23, 20u), 250u);  // mx < 2^(e_biased - 126)
       const float unit_inv = __uint_as_float((252u + 5u * kDigits - e_biased) << 23), u = 1.0f / unit_inv;
       float sum[2] = {0.0f, 0.0f};
-      f32x16 dig[kDigits][2];  // even and odd slots, as the packing conversion takes them
+      constexpr int kLower = kDigits == 4 ? 16 * (1 + 32 + 1024) : 16 * (1 + 32);  // lower digits offset to 0 .. 31
+      int v[32];
 #pragma unroll
-      for (int w = 0; w < 2; ++w)
+      for (int e = 0; e < 32; ++e) {
+        const float nf = rintf(x[e] * unit_inv);
+        sum[e >> 4] += nf * u;
+        v[e] = (int)nf + kLower;
+      }
 #pragma unroll
-        for (int f8 = 0; f8 < 2; ++f8)
+      for (int d = 0; d < kDigits; ++d) {
+        f32x16 dig[2];  // even and odd slots, as the packing conversion takes them
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {  // slot v of a lane is what ExpandF4 makes of the code words: word v / 16, field 2 (v % 8) + (v / 8) % 2
-            const float nf = rintf(x[8 * (2 * w + f8) + i] * unit_inv);
-            sum[w] += nf * u;
-            constexpr int kLower = kDigits == 4 ? 16 * (1 + 32 + 1024) : 16 * (1 + 32);
-            const int v = (int)nf + kLower, slot = 8 * (i & 1) + 4 * f8 + (i >> 1) + 16 * w;
-#pragma unroll
-            for (int d = 0; d < kDigits; ++d)
-              dig[d][slot & 1][slot >> 1] = 0.125f * (float)(d == kDigits - 1 ? v >> (5 * d) : ((v >> (5 * d)) & 31) - 16);
-          }
-#pragma unroll
-      for (int d = 0; d < kDigits; ++d)
-        digits[t][d] = __builtin_bit_cast(u32x6, __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(dig[d][0], dig[d][1], 1.0f));
+        for (int e = 0; e < 32; ++e) {
+          // slot of a lane: what ExpandF4 makes of the code words, word slot / 16, field 2 (slot % 8) + (slot / 8) % 2
+          const int i = e & 7, slot = 8 * (i & 1) + 4 * ((e >> 3) & 1) + (i >> 1) + 16 * (e >> 4);
+          dig[slot & 1][slot >> 1] = 0.125f * (float)(d == kDigits - 1 ? v[e] >> (5 * d) : ((v[e] >> (5 * d)) & 31) - 16);
+        }
+        digits[t][d] = __builtin_bit_cast(u32x6, __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(dig[0], dig[1], 1.0f));
+        asm volatile("" ::: "memory");  // one digit after the other: all of them at once take 128 registers
+      }
       if constexpr (NG == 2) {
         qsum[t][0] = column_sum(sum[0]);
         qsum[t][1] = column_sum(sum[1]);
       } else {
         qsum[t][0] = column_sum(sum[0] + sum[1]);
       }
-      unit_exp[t] = e_biased + 6u - 5u * kDigits;
+      unit_exp[t] = (e_biased + 6u - 5u * kDigits) * 0x01010101u + 0x0F0A0500u;  // a byte a digit: each 32 times the one below
     }
-    f32x4 acc_z[QT][NG];
+    // sums of weight * zero-point: one row of products serves all channels of a group, so rows 0-7 sum the first group's and rows 8-15
+    // the second's (lanes q = 0, 1 and 2, 3 of the result)
+    f32x4 acc_z[QT];
 #pragma unroll
-    for (int t = 0; t < QT; ++t)
-#pragma unroll
-      for (int g = 0; g < NG; ++g) acc_z[t][g] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < QT; ++t) acc_z[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
     BlockMeta<NG> &bm = sh.meta[wave];
+    if (NG == 2 && lane < 32) bm.none[lane] = 0;
+    const uint16_t *zero_at[2][NG];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int g = 0; g < NG; ++g) zero_at[x][g] = NG == 1 || n / 8 == g ? &bm.v_zero[x][g][8 * q] : &bm.none[8 * q];
     const ExpandF4 ex4;
     const int32_t *table = c.table + (size_t)b * c.max_pages;
     auto page_of = [&](int blk) { return table[min(blk * 32, s.len - 1) >> c.page_shift]; };
-    auto load_block = [&](int blk, int page, CodeBlock<NG> &t) {
+    struct Where { size_t row; int limit; };  // first row of a block in the pools; rows from `limit` on (of the sequence) take no part
+    auto find = [&](int blk, int page) {
       const bool there = page >= 0 && page < c.n_pages;
-      const int in_page = (blk * 32) & ((1 << c.page_shift) - 1);
-      const size_t row = (((size_t)(there ? page : 0) * c.Hkv + head) << c.page_shift) + in_page;
-      t.limit = there ? s.len : 0;
-      t.k = *reinterpret_cast<const u32x4 *>(c.k_codes + row / 32 * kBlockWords + 4 * lane);
-      t.v = *reinterpret_cast<const u32x4 *>(c.v_codes + row / 32 * kBlockWords + 4 * lane);
-      const uint32_t *meta = (lane < 32 ? c.k_meta : c.v_meta) + (row + (lane & 31)) * NG;
+      return Where{(((size_t)(there ? page : 0) * c.Hkv + head) << c.page_shift) + ((blk * 32) & ((1 << c.page_shift) - 1)), there ? s.len : 0};
+    };
+    auto load_meta = [&](const Where &at, CodeBlock<NG> &t) {
+      const uint32_t *meta = (lane < 32 ? c.k_meta : c.v_meta) + (at.row + (lane & 31)) * NG;
       if constexpr (NG == 2) {
         const u32x2 w = *reinterpret_cast<const u32x2 *>(meta);
         t.meta[0] = w[0]; t.meta[1] = w[1];
       } else {
         t.meta[0] = *meta;
       }
+      t.limit = at.limit;
     };
-    auto process = [&](const CodeBlock<NG> &cur, int blk) {
+    auto load_keys = [&](const Where &at, CodeBlock<NG> &t) { t.k = *reinterpret_cast<const u32x4 *>(c.k_codes + at.row * 8 + 4 * lane); };
+    auto load_values = [&](const Where &at, CodeBlock<NG> &t) { t.v = *reinterpret_cast<const u32x4 *>(c.v_codes + at.row * 8 + 4 * lane); };
+    // one block; done_meta, done_keys, done_values: called when that part of `cur` has been taken
+    auto process = [&](CodeBlock<NG> &cur, int blk, auto &&done_meta, auto &&done_keys, auto &&done_values) {
       // ---- meta words: a row a lane
       bool far = false;  // a zero-point that 11 bits do not hold
       {
@@ -346,83 +379,77 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(Paged
       }
       const bool any_far = __ballot(far) != 0ull;
       wave_lds_sync();
-      f32x4 k_scale[NG][2], k_zero[NG][2], v_log[2], v_rcp[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          k_scale[g][h] = *reinterpret_cast<const f32x4 *>(&bm.k_scale[g][16 * h + 4 * q]);
-          k_zero[g][h] = *reinterpret_cast<const f32x4 *>(&bm.k_zero[g][16 * h + 4 * q]);
-        }
-        v_log[h] = *reinterpret_cast<const f32x4 *>(&bm.v_log[16 * h + 4 * q]);
-        v_rcp[h] = *reinterpret_cast<const f32x4 *>(&bm.v_rcp[16 * h + 4 * q]);
-      }
+      done_meta();
       // ---- scores and weights
-      u32x4 codes[2][NG];
+      float y[QT][2][4];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const u32x2 lo = ex4(cur.k[2 * h]), hi = ex4(cur.k[2 * h + 1]);
-        if constexpr (NG == 2) {
-          codes[h][0] = (u32x4){lo[0], lo[1], 0u, 0u};
-          codes[h][1] = (u32x4){0u, 0u, hi[0], hi[1]};
+        u32x4 codes[NG];
+        f32x4 k_scale[NG], k_zero[NG];
+        const f32x4 v_log = *reinterpret_cast<const f32x4 *>(&bm.v_log[16 * h + 4 * q]);
+        if constexpr (NG == 2) {  // a group's product takes zeros in the other group's slots
+          codes[0] = (u32x4){lo[0], lo[1], 0u, 0u};
+          codes[1] = (u32x4){0u, 0u, hi[0], hi[1]};
         } else {
-          codes[h][0] = (u32x4){lo[0], lo[1], hi[0], hi[1]};
+          codes[0] = (u32x4){lo[0], lo[1], hi[0], hi[1]};
         }
-      }
-      u32x4 w[QT][NG];
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        float y[2][4];
+        for (int g = 0; g < NG; ++g) {
+          k_scale[g] = *reinterpret_cast<const f32x4 *>(&bm.k_scale[g][16 * h + 4 * q]);
+          k_zero[g] = *reinterpret_cast<const f32x4 *>(&bm.k_zero[g][16 * h + 4 * q]);
+        }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int t = 0; t < QT; ++t) {
           f32x4 acc[NG];
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
             acc[g] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int d = 0; d < kDigits; ++d) acc[g] = mfma_codes(codes[h][g], digits[t][d], unit_exp[t] + 5u * d, acc[g]);
+            acc[g] = mfma_codes<0>(codes[g], digits[t][0], unit_exp[t], acc[g]);
+            acc[g] = mfma_codes<1>(codes[g], digits[t][1], unit_exp[t], acc[g]);
+            acc[g] = mfma_codes<2>(codes[g], digits[t][2], unit_exp[t], acc[g]);
+            if constexpr (kDigits == 4) acc[g] = mfma_codes<kDigits - 1>(codes[g], digits[t][kDigits - 1], unit_exp[t], acc[g]);
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float v = v_log[h][i];
+            float v = v_log[i];
 #pragma unroll
             for (int g = 0; g < NG; ++g)
-              v = __builtin_fmaf(k_scale[g][h][i], __builtin_fmaf(-k_zero[g][h][i], qsum[t][g], acc[g][i]), v);
-            y[h][i] = v;
+              v = __builtin_fmaf(k_scale[g][i], __builtin_fmaf(-k_zero[g][i], qsum[t][g], acc[g][i]), v);
+            y[t][h][i] = v;
           }
         }
-        weigh(t, y, [&](float alpha) {
+      }
+      done_keys();
+      u32x4 w[QT][NG];
+      const f32x4 r0 = *reinterpret_cast<const f32x4 *>(&bm.v_rcp[4 * q]), r1 = *reinterpret_cast<const f32x4 *>(&bm.v_rcp[16 + 4 * q]);
 #pragma unroll
-          for (int g = 0; g < NG; ++g) acc_z[t][g] *= alpha;
-        });
+      for (int t = 0; t < QT; ++t) {
+        weigh(t, y[t], [&](float alpha) { acc_z[t] *= alpha; });
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) l[t] = __builtin_fmaf(y[h][i], v_rcp[h][i], l[t]);
+        for (int i = 0; i < 4; ++i) l[t] = __builtin_fmaf(y[t][0][i], r0[i], __builtin_fmaf(y[t][1][i], r1[i], l[t]));
         if constexpr (NG == 2) {
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
             const f32x4 s0 = *reinterpret_cast<const f32x4 *>(&bm.v_share[g][4 * q]), s1 = *reinterpret_cast<const f32x4 *>(&bm.v_share[g][16 + 4 * q]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[t][g][i] = pack_f16x2(y[0][i] * s0[i], y[1][i] * s1[i]);
+            for (int i = 0; i < 4; ++i) w[t][g][i] = pack_f16x2(y[t][0][i] * s0[i], y[t][1][i] * s1[i]);
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[t][0][i] = pack_f16x2(y[0][i], y[1][i]);
+          for (int i = 0; i < 4; ++i) w[t][0][i] = pack_f16x2(y[t][0][i], y[t][1][i]);
         }
       }
       // ---- values
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const u32x4 z = *reinterpret_cast<const u32x4 *>(&bm.v_zero[0][g][8 * q]);
+      for (int x = 0; x < 2; ++x)
+        if (x == 0 || any_far)
 #pragma unroll
-        for (int t = 0; t < QT; ++t) acc_z[t][g] = mfma_f16(z, w[t][g], acc_z[t][g]);
-        if (any_far) {
-          const u32x4 z2 = *reinterpret_cast<const u32x4 *>(&bm.v_zero[1][g][8 * q]);
+          for (int g = 0; g < NG; ++g) {
+            const u32x4 z = *reinterpret_cast<const u32x4 *>(zero_at[x][g]);
 #pragma unroll
-          for (int t = 0; t < QT; ++t) acc_z[t][g] = mfma_f16(z2, w[t][g], acc_z[t][g]);
-        }
-      }
+            for (int t = 0; t < QT; ++t) acc_z[t] = mfma_f16(z, w[t][g], acc_z[t]);
+          }
 #pragma unroll
       for (int wd = 0; wd < 4; ++wd) {
         const int g = NG == 2 ? (wd & 1) : 0, nb = 4 * (wd & 1) + (wd >> 1);
@@ -435,34 +462,84 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(Paged
           o[t][nb + 2] = mfma_f16(vy, w[t][g], o[t][nb + 2]);
         }
       }
+      done_values();
       wave_lds_sync();  // the next block's meta words overwrite this one's
     };
-    // a block is requested while the one before it is worked on, its page's number one block earlier
-    CodeBlock<NG> buf[2];
+    // The next block is requested while one is worked on, and its page's number one block earlier.  Many rows: each part into its own
+    // registers as soon as they are free (another set would be ten too many); few rows, bound by the stream: all of it at once.
     const int first = u0 + wk;
-    load_block(first, page_of(first), buf[0]);
-    int next_page = page_of(min(first + WK, n_code - 1));
-    for (int blk = first; blk < code_end; blk += 2 * WK) {
+    Where at = find(first, page_of(first));
+    int page = page_of(min(first + WK, n_code - 1));
+    CodeBlock<NG> buf[MANY ? 1 : 2];
+    load_meta(at, buf[0]);
+    load_keys(at, buf[0]);
+    load_values(at, buf[0]);
+    if constexpr (MANY) {
+      for (int blk = first; blk < code_end; ++blk) {
+        at = find(min(blk + 1, n_code - 1), page);
+        page = page_of(min(blk + 2, n_code - 1));
+        process(buf[0], blk, [&] { load_meta(at, buf[0]); }, [&] { load_keys(at, buf[0]); }, [&] { load_values(at, buf[0]); });
+      }
+    } else {
+      for (int blk = first; blk < code_end; blk += 2 * WK) {
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int now = blk + x * WK;
-        if (now >= code_end) break;
-        load_block(min(now + WK, n_code - 1), next_page, buf[1 - x]);
-        next_page = page_of(min(now + 2 * WK, n_code - 1));
-        process(buf[x], now);
+        for (int x = 0; x < 2; ++x) {
+          const int now = blk + x * WK;
+          if (now >= code_end) break;
+          at = find(min(now + WK, n_code - 1), page);
+          page = page_of(min(now + 2 * WK, n_code - 1));
+          load_meta(at, buf[1 - x]);
+          load_keys(at, buf[1 - x]);
+          load_values(at, buf[1 - x]);
+          process(buf[x], now, [] {}, [] {}, [] {});
+        }
       }
     }
 #pragma unroll
-    for (int t = 0; t < QT; ++t)
+    for (int t = 0; t < QT; ++t) {
+      const float mine = -64.0f * acc_z[t][0], other = NG == 2 ? __shfl_xor(mine, 32, kWave) : mine;
+      const float z[2] = {q < 2 ? mine : other, q < 2 ? other : mine};
 #pragma unroll
       for (int nb = 0; nb < 8; ++nb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[t][nb][i] = __builtin_fmaf(o[t][nb][i], 16777216.0f, -64.0f * acc_z[t][NG == 2 ? nb / 4 : 0][i]);
+        for (int i = 0; i < 4; ++i) o[t][nb][i] = __builtin_fmaf(o[t][nb][i], 16777216.0f, z[NG == 2 ? nb / 4 : 0]);
+    }
   }
+
+  // Sixteen-bit keys and values of a workgroup of many rows go through LDS, a stage at a time: every thread brings two chunks of keys
+  // and of values, asked for while the stage before is worked on.  `from(key?, row, chunk)`: where a chunk comes from.
+  [[maybe_unused]] auto staged = [&](int begin, int end, auto &&from, auto &&at_v, auto &&work) {  // stages [begin, end), uniform over the workgroup
+    if constexpr (MANY) {
+      if (begin >= end) return;
+      u32x4 kx[2], vx[2];
+      auto ask = [&](int stage) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int id = threadIdx.x + 512 * x, row = id >> 4, chunk = id & 15;
+          kx[x] = *reinterpret_cast<const u32x4 *>(from(true, stage, row, chunk));
+          vx[x] = *reinterpret_cast<const u32x4 *>(from(false, stage, row, chunk));
+        }
+      };
+      ask(begin);
+      for (int stage = begin; stage < end; ++stage) {
+        const int buf = stage & 1;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int id = threadIdx.x + 512 * x, row = id >> 4, chunk = id & 15;
+          *reinterpret_cast<u32x4 *>(&sh.k[buf][staged_at(row, chunk)]) = kx[x];
+          *reinterpret_cast<u32x4 *>(&sh.v[buf][at_v(row, chunk)]) = vx[x];
+        }
+        if (stage + 1 < end) ask(stage + 1);
+        lds_barrier();  // (the other buffer was last read in front of the barrier before)
+        work(stage, buf);
+      }
+      lds_barrier();  // whoever comes next overwrites the stages
+    }
+  };
 
   // ================= 16-bit rows of the cache =================
   const int wide_begin = max(u0 - n_code, 0), wide_end = min(u1 - n_code, n_wide);
-  if (!idle && wide_begin + wk < wide_end) {
+  if (wide_begin < wide_end) {
     u32x4 q_hi[QT][4], q_lo[QT][4];  // two bfloat16 terms: 16 bits of the query
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -479,44 +556,64 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(Paged
         }
     }
     const uint16_t *ks = c.k_sal + (size_t)unit * c.S_cap * kD, *vs = c.v_sal + (size_t)unit * c.S_cap * kD;
-    for (int blk = wide_begin + wk; blk < wide_end; blk += WK) {
-      u32x4 k[2][4];
+    // one block of 32 slots; key(h, ch), value(nb): operands
+    auto wide_block = [&](int blk, auto &&key, auto &&value) {
+      u32x4 hi[QT], lo[QT];
+      float y[QT][2][4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h) {
+        f32x4 acc[QT];
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch)
-          k[h][ch] = *reinterpret_cast<const u32x4 *>(ks + (size_t)(blk * 32 + 16 * h + n) * kD + 32 * ch + 8 * q);
-      u32x4 v[8];
+        for (int t = 0; t < QT; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int nb = 0; nb < 8; ++nb) {
-        v[nb] = *reinterpret_cast<const u32x4 *>(vs + (size_t)blk * 4096 + nb * 512 + 8 * lane);
-        if (blk * 32 + 32 > wide)  // slots behind the last row may hold anything, and 0 * NaN is no 0
+        for (int ch = 0; ch < 4; ++ch) {
+          const u32x4 k = key(h, ch);
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            v[nb][i] &= (blk * 32 + 4 * q + i < wide ? 0xFFFFu : 0u) | (blk * 32 + 16 + 4 * q + i < wide ? 0xFFFF0000u : 0u);
+          for (int t = 0; t < QT; ++t) acc[t] = mfma_b16(k, q_hi[t][ch], mfma_b16(k, q_lo[t][ch], acc[t]));
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[t][h][i] = blk * 32 + 16 * h + 4 * q + i < wide ? acc[t][i] : -INFINITY;
       }
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        float y[2][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int ch = 0; ch < 4; ++ch) acc = mfma_b16(k[h][ch], q_hi[t][ch], mfma_b16(k[h][ch], q_lo[t][ch], acc));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[h][i] = blk * 32 + 16 * h + 4 * q + i < wide ? acc[i] : -INFINITY;
-        }
-        weigh(t, y, [](float) {});
-        u32x4 hi, lo;
+        weigh(t, y[t], [](float) {});
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          l[t] += y[0][i] + y[1][i];
-          hi[i] = pack_bf16x2(y[0][i], y[1][i]);
-          lo[i] = pack_bf16x2(y[0][i] - __uint_as_float(hi[i] << 16), y[1][i] - __uint_as_float(hi[i] & 0xFFFF0000u));
+          l[t] += y[t][0][i] + y[t][1][i];
+          hi[t][i] = pack_bf16x2(y[t][0][i], y[t][1][i]);
+          lo[t][i] = pack_bf16x2(y[t][0][i] - __uint_as_float(hi[t][i] << 16), y[t][1][i] - __uint_as_float(hi[t][i] & 0xFFFF0000u));
         }
-#pragma unroll
-        for (int nb = 0; nb < 8; ++nb) o[t][nb] = mfma_b16(v[nb], hi, mfma_b16(v[nb], lo, o[t][nb]));
       }
+#pragma unroll
+      for (int nb = 0; nb < 8; ++nb) {
+        u32x4 v = value(nb);
+        if (blk * 32 + 32 > wide)  // slots behind the last row may hold anything, and 0 * NaN is no 0
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            v[i] &= (blk * 32 + 4 * q + i < wide ? 0xFFFFu : 0u) | (blk * 32 + 16 + 4 * q + i < wide ? 0xFFFF0000u : 0u);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) o[t][nb] = mfma_b16(v, hi[t], mfma_b16(v, lo[t], o[t][nb]));
+      }
+    };
+    if constexpr (MANY) {
+      staged(wide_begin / 2, (wide_end + 1) / 2,
+             [&](bool key, int stage, int row, int chunk) { return (key ? ks : vs) + (size_t)stage * (kStage * kD) + row * kD + 8 * chunk; },
+             [](int row, int chunk) { return row * kD + 8 * chunk; },  // (tiles: a wavefront reads 1 KB pieces as they lie)
+             [&](int stage, int buf) {
+               if (idle) return;
+#pragma unroll
+               for (int x = 0; x < 2; ++x)
+                 if (2 * stage + x >= wide_begin && 2 * stage + x < wide_end)
+                   wide_block(2 * stage + x,
+                              [&](int h, int ch) { return *reinterpret_cast<const u32x4 *>(&sh.k[buf][staged_at(32 * x + 16 * h + n, 4 * ch + q)]); },
+                              [&](int nb) { return *reinterpret_cast<const u32x4 *>(&sh.v[buf][x * 4096 + nb * 512 + 8 * lane]); });
+             });
+    } else {
+      for (int blk = wide_begin + wk; blk < wide_end; blk += WK)
+        wide_block(blk, [&](int h, int ch) { return *reinterpret_cast<const u32x4 *>(ks + (size_t)(blk * 32 + 16 * h + n) * kD + 32 * ch + 8 * q); },
+                   [&](int nb) { return *reinterpret_cast<const u32x4 *>(vs + (size_t)blk * 4096 + nb * 512 + 8 * lane); });
     }
   }
   // The cached rows' share is rotated back (H is its own inverse), and the chunk's rows join it.  Their weights are relative to the
@@ -537,53 +634,55 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(Paged
   }
 
   // ================= rows of the chunk =================
-  const int self_begin = max(u0 - n_code - n_wide, 0);
-  int self_end = min(u1 - n_code - n_wide, n_self);
-  const int low_token = row0 / R;                                             // of this wavefront's rows
-  self_end = min(self_end, (min(row0 + kRows, rows) - 1) / R / 32 + 1);       // (before an idle wavefront's first row: nothing to do)
-  if (!idle) {
-    auto &vt = sh.v[wave];
+  const int self_begin = max(u0 - n_code - n_wide, 0), self_end = min(u1 - n_code - n_wide, n_self);
+  if (self_begin < self_end) {
+    const int low_token = row0 / R;                                        // of this wavefront's rows
+    const int my_end = idle ? 0 : (min(row0 + kRows, rows) - 1) / R / 32 + 1;
     const uint16_t *ks = a.k + s.first * a.k_stride + head * kD, *vs = a.v + s.first * a.v_stride + head * kD;
     int token[QT];
+    u32x4 raw[QT][4];
 #pragma unroll
-    for (int t = 0; t < QT; ++t) token[t] = min(row0 + 16 * t + n, rows - 1) / R;
-    for (int blk = self_begin + wk; blk < self_end; blk += WK) {
-      u32x4 k[2][4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int ch = 0; ch < 4; ++ch)
-          k[h][ch] = *reinterpret_cast<const u32x4 *>(ks + min(blk * 32 + 16 * h + n, s.rows - 1) * a.k_stride + 32 * ch + 8 * q);
-#pragma unroll
-      for (int x = 0; x < 8; ++x)
-        *reinterpret_cast<u32x4 *>(&vt[4 * x + q][8 * n]) =
-            *reinterpret_cast<const u32x4 *>(vs + min(blk * 32 + 4 * x + q, s.rows - 1) * a.v_stride + 8 * n);
-      wave_lds_sync();
+    for (int t = 0; t < QT; ++t) {
+      token[t] = min(row0 + 16 * t + n, rows - 1) / R;
+      load_query(t, raw[t]);
+    }
+    // one block of 32 rows; key(h, ch): operand; vt, vrow: where the block's values lie in LDS
+    auto self_block = [&](int blk, auto &&key, const uint16_t *vt, int vrow) {
       u32x4 w[QT];
+      float y[QT][2][4];
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        float y[2][4];
+      for (int h = 0; h < 2; ++h) {
+        f32x4 acc[QT];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < QT; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int ch = 0; ch < 4; ++ch) acc = mfma_f16(k[h][ch], raw[t][ch], acc);
+        for (int ch = 0; ch < 4; ++ch) {
+          const u32x4 k = key(h, ch);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) y[h][i] = acc[i] * sm2;
+          for (int t = 0; t < QT; ++t) acc[t] = mfma_f16(k, raw[t][ch], acc[t]);
         }
-        if (blk * 32 + 31 > low_token) {  // uniform over the wavefront: some row may not look at all of the block
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[t][h][i] = acc[t][i] * sm2;
+      }
+      if (blk * 32 + 31 > low_token) {  // uniform over the wavefront: some row may not look at all of the block
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (blk * 32 + 16 * h + 4 * q + i > token[t]) y[h][i] = -INFINITY;
-        }
-        weigh(t, y, [](float) {});
+              if (blk * 32 + 16 * h + 4 * q + i > token[t]) y[t][h][i] = -INFINITY;
+      }
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        weigh(t, y[t], [](float) {});
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          l[t] += (y[h][0] + y[h][1]) + (y[h][2] + y[h][3]);
-          w[t][2 * h] = pack_f16x2(y[h][0], y[h][1]);
-          w[t][2 * h + 1] = pack_f16x2(y[h][2], y[h][3]);
+          l[t] += (y[t][h][0] + y[t][h][1]) + (y[t][h][2] + y[t][h][3]);
+          w[t][2 * h] = pack_f16x2(y[t][h][0], y[t][h][1]);
+          w[t][2 * h + 1] = pack_f16x2(y[t][h][2], y[t][h][3]);
         }
       }
 #pragma unroll
@@ -592,14 +691,43 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(Paged
 #pragma unroll
         for (int h = 0; h < 2; ++h) {  // a transposing read: the lane gets its channel of rows 16h + 4q .. + 3
           const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4 *)(&vt[16 * h + 4 * q + (n >> 2)][16 * nb + 4 * (n & 3)])));
+              (__attribute__((address_space(3))) s16x4 *)(&vt[staged_at(vrow + 16 * h + 4 * q + (n >> 2), 2 * nb + ((n & 3) >> 1)) + 4 * (n & 1)])));
           v[2 * h] = x[0];
           v[2 * h + 1] = x[1];
         }
 #pragma unroll
         for (int t = 0; t < QT; ++t) o[t][nb] = mfma_f16(v, w[t], o[t][nb]);
       }
-      wave_lds_sync();
+    };
+    if constexpr (MANY) {
+      staged(self_begin / 2, (self_end + 1) / 2,
+             [&](bool key, int stage, int row, int chunk) {
+               const int r = min(stage * kStage + row, s.rows - 1);
+               return (key ? ks + r * a.k_stride : vs + r * a.v_stride) + 8 * chunk;
+             },
+             staged_at,
+             [&](int stage, int buf) {
+#pragma unroll
+               for (int x = 0; x < 2; ++x) {
+                 const int blk = 2 * stage + x;
+                 if (blk >= self_begin && blk < min(self_end, my_end))
+                   self_block(blk, [&](int h, int ch) { return *reinterpret_cast<const u32x4 *>(&sh.k[buf][staged_at(32 * x + 16 * h + n, 4 * ch + q)]); },
+                              sh.v[buf], 32 * x);
+               }
+             });
+    } else {
+      uint16_t *vt = sh.v[wave];
+      for (int blk = self_begin + wk; blk < min(self_end, my_end); blk += WK) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          *reinterpret_cast<u32x4 *>(&vt[staged_at(4 * x + q, n)]) =
+              *reinterpret_cast<const u32x4 *>(vs + min(blk * 32 + 4 * x + q, s.rows - 1) * a.v_stride + 8 * n);
+        wave_lds_sync();
+        self_block(blk, [&](int h, int ch) {
+          return *reinterpret_cast<const u32x4 *>(ks + min(blk * 32 + 16 * h + n, s.rows - 1) * a.k_stride + 32 * ch + 8 * q);
+        }, vt, 0);
+        wave_lds_sync();
+      }
     }
   }
 
@@ -620,7 +748,7 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(Paged
       if (ch == 0) { p[0] = top; p[1] = sum; }
     }
   };
-  if constexpr (WK == 1) {
+  if constexpr (MANY) {
     if (idle) return;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -637,7 +765,7 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attention_kernel(Paged
       if (q == 0) { sh.m[wk][16 * t + n] = m[t]; sh.l[wk][16 * t + n] = l[t]; }
     }
     __syncthreads();
-    for (int at = threadIdx.x; at < kRows * 32; at += 64 * kPagedWaves) {
+    for (int at = threadIdx.x; at < kRows * 32; at += 64 * NW) {
       const int r = at >> 5, ch = 4 * (at & 31);
       if (row0 + r >= rows) break;
       float top = sh.m[0][r], sum = 0.0f;
@@ -682,10 +810,10 @@ template <int G>
 void launch_variant(const PagedAttentionArgs &a, int rows, hipStream_t stream) {
   const int units = a.c.B * a.c.Hkv;
   auto grid = [&](int per) { return dim3((rows + per - 1) / per, units, a.n_split); };
-  const dim3 block(64 * kPagedWaves);
-  if (rows <= 16) paged_attention_kernel<G, 1, 4><<<grid(16), block, 0, stream>>>(a);
-  else if (rows <= 64) paged_attention_kernel<G, 2, 4><<<grid(32), block, 0, stream>>>(a);
-  else paged_attention_kernel<G, 2, 1><<<grid(128), block, 0, stream>>>(a);
+  constexpr int kFew = 64 * kFewWaves, kMany = 64 * kManyWaves;
+  if (rows <= 16) paged_attention_kernel<G, 1, false><<<grid(16), kFew, 0, stream>>>(a);
+  else if (rows <= 64) paged_attention_kernel<G, 2, false><<<grid(32), kFew, 0, stream>>>(a);
+  else paged_attention_kernel<G, 2, true><<<grid(32 * kManyWaves), kMany, 0, stream>>>(a);
 }
 
 }  // namespace
