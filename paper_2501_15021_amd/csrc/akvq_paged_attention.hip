@@ -11,7 +11,9 @@
 // wavefront, a row a lane) and the chunk's V rows (transposed by the reads).
 //   K codes enter the scaled 16x16x128 product as 4-bit floats without decoding (three instructions per 16 codes), against the query as
 // kDigits balanced base-32 digits that 6-bit floats hold exactly: 5 * kDigits bits of the query's largest channel, at the price of
-// kDigits / 4 of a 16-bit product.  Scale and zero-point of a row are applied to its score.
+// kDigits / 4 of a 16-bit product.  What else a score holds comes from one more product, that the codes' products are added onto: per row
+// zero-point, 1 / scale and log2(V scale) / scale, per column the query's sum, the reference and 1, all in bfloat16 terms that
+// together hold the 32-bit numbers.  One multiplication by the row's scale is left.
 //   V codes are masked in place, which leaves binary16 subnormals code * 4^ii * 2^-24 (ii: the row's place in its word): one
 // instruction per two codes.  The V scale and 4^-ii ride in the exponent of the weight, the denominator takes the weight back by
 // 4^ii / scale, and zero-points are summed by one more product.  What is left to the vector units is the softmax, which bounds the
@@ -27,7 +29,7 @@ namespace {
 constexpr int kDigits = 4;  // 3 or 4
 constexpr int kFewWaves = 4;   // of a workgroup that has few rows: they share them and deal the keys among them
 constexpr int kManyWaves = 8;  // of a workgroup that has many: each has its own, and all look at the same keys
-constexpr float kNoScore = -1.0e30f;   // reference before the first score
+constexpr float kNoScore = -1.0e30f;   // score of a row that takes no part, reference of a column without scores
 constexpr float kRaiseAt = 15.0f;      // a score may exceed the reference by this (2^15 is the largest weight) ...
 constexpr float kRaiseTo = 7.0f;       // ... and then gets a reference this far below it
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -126,15 +128,33 @@ __device__ __forceinline__ void wht128_output(f32x4 (&o)[8], int q) {
   for (int nb = 0; nb < 8; ++nb) o[nb] *= inv_sqrt128();
 }
 
-// What a wavefront decodes of a block's meta words, a row a lane, for all its columns.
+// A float as three bfloat16 terms (its 24 bits), in the upper halves.
+struct Terms { float a, b, c; };
+__device__ __forceinline__ Terms split_terms(float v) {
+  Terms t;
+  t.a = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
+  const float r = v - t.a;
+  t.b = __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
+  t.c = r - t.b;
+  return t;
+}
+__device__ __forceinline__ uint32_t upper_halves(float lo, float hi) {
+  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+}
+
+// What is decoded of a block's meta words, a row a lane, for all columns that look at the block.
 template <int NG>
 struct BlockMeta {
-  float k_scale[NG][32], k_zero[NG][32];  // a row that takes no part: 0
-  float v_log[32];                        // log2(scale) - 2 ii, of the larger scale where there are two (no part: -inf)
-  float v_rcp[32];                        // 4^ii / that scale (no part: 0)
-  float v_share[NG][32];                  // scale / that scale (two groups only)
-  uint16_t v_zero[2][NG][32];             // binary16, in the weights' order: zero-point * 4^(ii - 3), low part and multiples of 2048
-  uint16_t none[32];                      // zeros (two groups only)
+  // Row operands of the product that a score starts with, eight bfloat16 slots for each lane group q.  q = 0: -zero-point (low byte and
+  // multiples of 256, three times each: times the three terms of the query's sum).  q = 1: terms of 1 / scale (times those of minus the reference).
+  // q = 2: terms of log2(V scale) / scale - 2 ii / scale (times 1); a row that takes no part has kNoScore here, a scale of 1 and no other terms.
+  __attribute__((aligned(16))) uint16_t start[32][4][8];
+  __attribute__((aligned(16))) uint16_t start2[NG == 2 ? 32 : 1][8];  // q = 3, of the second group's product: its zero-point (the query's sum over it)
+  __attribute__((aligned(16))) float k_scale[NG][32];
+  __attribute__((aligned(16))) float v_rcp[32];                       // 4^ii / V scale, the larger one where there are two (no part: 0)
+  __attribute__((aligned(16))) float v_share[NG == 2 ? 2 : 1][32];    // V scale / the larger one
+  __attribute__((aligned(16))) uint16_t v_zero[2][NG][32];            // binary16, in the weights' order: zero-point * 4^(ii - 3), low part and multiples of 2048
+  int far;                                                            // some zero-point has such multiples
 };
 
 template <int NG>
@@ -159,15 +179,17 @@ template <int G, int QT, bool MANY>
 struct PagedShared;
 template <int G, int QT>
 struct PagedShared<G, QT, true> {
-  BlockMeta<kD / G> meta[kManyWaves];
+  BlockMeta<kD / G> meta[2][kManyWaves];  // of the blocks being worked on, and the next
   __attribute__((aligned(16))) uint16_t k[2][kStage * kD], v[2][kStage * kD];
+  __attribute__((aligned(16))) uint16_t none[32];
 };
 template <int G, int QT>
 struct PagedShared<G, QT, false> {
-  BlockMeta<kD / G> meta[kFewWaves];
+  BlockMeta<kD / G> meta[1][kFewWaves];
   __attribute__((aligned(16))) uint16_t v[kFewWaves][32 * kD];
   __attribute__((aligned(16))) float o[kFewWaves][16 * QT][kD + 4];
   float m[kFewWaves][16 * QT], l[kFewWaves][16 * QT];
+  __attribute__((aligned(16))) uint16_t none[32];
 };
 
 template <int G, int QT, bool MANY>
@@ -206,13 +228,16 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
   decode_split_range(n_code + n_wide + n_self, a.n_split, split, u0, u1);
 
   f32x4 o[QT][8];
-  float m[QT], l[QT];
+  // per column: the reference that weights are relative to, from which excess over it it is raised (before the first score: any), and
+  // this lane's share of the sum
+  float m[QT], limit[QT], l[QT];
   const uint16_t *q_at[QT];  // of this lane's column
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
 #pragma unroll
     for (int nb = 0; nb < 8; ++nb) o[t][nb] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    m[t] = kNoScore;
+    m[t] = 0.0f;
+    limit[t] = 0.5f * kNoScore;
     l[t] = 0.0f;
     const int row = min(row0 + 16 * t + n, rows - 1), token = row / R;
     q_at[t] = a.q + (s.first + token) * a.q_stride + (head * R + row - token * R) * kD + 8 * q;
@@ -242,37 +267,49 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 #pragma unroll
     for (int e = 0; e < 32; ++e) x[e] *= f;
   };
-  // Weights of a tile's eight scores (rows 4q + i of the two halves of a block; -inf: no part).  The reference of a column is raised, and what
-  // was summed against it rescaled by `more`, only when a score exceeds it by kRaiseAt.
+  // Weights of a tile's eight scores relative to the reference (rows 4q + i of the two halves of a block; no part: far below).  The
+  // reference is raised, and what was summed against it rescaled (`more`: the rest of it), only when a score exceeds it by kRaiseAt.
   auto weigh = [&](int t, float (&y)[2][4], auto &&more) {
     float top = y[0][0];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, y[h][i]);
-    if (__ballot(top > m[t] + kRaiseAt) != 0ull) {
+    if (__ballot(top > limit[t]) != 0ull) {
       const float all = column_max(top);
-      if (all > m[t] + kRaiseAt) {
-        const float alpha = exp2_bare(m[t] - (all - kRaiseTo));  // 0 while there was no score
+      float by = 0.0f;
+      if (all > limit[t]) {  // the four lanes of a column agree
+        const float to = rintf(m[t] + all) - kRaiseTo;
+        by = to - m[t];
+        const float alpha = limit[t] < 0.0f ? 0.0f : exp2_bare(-by);  // (there was nothing before the first score)
 #pragma unroll
         for (int nb = 0; nb < 8; ++nb) o[t][nb] *= alpha;
         l[t] *= alpha;
+        m[t] = to;
+        limit[t] = kRaiseAt;
         more(alpha);
-        m[t] = all - kRaiseTo;
       }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[h][i] -= by;
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[h][i] = exp2_bare(y[h][i] - m[t]);
+      for (int i = 0; i < 4; ++i) y[h][i] = exp2_bare(y[h][i]);
   };
 
   // ================= code rows =================
   const int code_end = min(u1, n_code);
-  if (!idle && u0 + wk < code_end) {
+  if (MANY ? u0 < code_end : u0 + wk < code_end) {
     u32x6 digits[QT][kDigits];
     uint32_t unit_exp[QT];
-    float qsum[QT][NG];
+    u32x4 start[QT];  // column operands of the first product: terms of the query's sums, of minus the reference, ones
+    auto start_slots = [&](float v) {
+      const Terms x = split_terms(v);
+      return (u32x4){upper_halves(x.a, x.b), upper_halves(x.c, x.a), upper_halves(x.b, q == 1 ? x.a : x.c), 0u};
+    };
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       float x[32], mx = 0.0f;
@@ -304,12 +341,16 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
         digits[t][d] = __builtin_bit_cast(u32x6, __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(dig[0], dig[1], 1.0f));
         asm volatile("" ::: "memory");  // one digit after the other: all of them at once take 128 registers
       }
+      float qs = 0.0f;
       if constexpr (NG == 2) {
-        qsum[t][0] = column_sum(sum[0]);
-        qsum[t][1] = column_sum(sum[1]);
+        const float s0 = column_sum(sum[0]), s1 = column_sum(sum[1]);
+        qs = q == 0 ? s0 : q == 3 ? s1 : 0.0f;
       } else {
-        qsum[t][0] = column_sum(sum[0] + sum[1]);
+        const float s0 = column_sum(sum[0] + sum[1]);
+        qs = q == 0 ? s0 : 0.0f;
       }
+      start[t] = start_slots(qs);
+      if (q == 2) start[t] = (u32x4){0x3F803F80u, 0x00003F80u, 0u, 0u};
       unit_exp[t] = (e_biased + 6u - 5u * kDigits) * 0x01010101u + 0x0F0A0500u;  // a byte a digit: each 32 times the one below
     }
     // sums of weight * zero-point: one row of products serves all channels of a group, so rows 0-7 sum the first group's and rows 8-15
@@ -318,13 +359,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 #pragma unroll
     for (int t = 0; t < QT; ++t) acc_z[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
-    BlockMeta<NG> &bm = sh.meta[wave];
-    if (NG == 2 && lane < 32) bm.none[lane] = 0;
-    const uint16_t *zero_at[2][NG];
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int g = 0; g < NG; ++g) zero_at[x][g] = NG == 1 || n / 8 == g ? &bm.v_zero[x][g][8 * q] : &bm.none[8 * q];
+    if (lane < 16) reinterpret_cast<uint32_t *>(sh.none)[lane] = 0u;  // (by every wavefront for itself)
     const ExpandF4 ex4;
     const int32_t *table = c.table + (size_t)b * c.max_pages;
     auto page_of = [&](int blk) { return table[min(blk * 32, s.len - 1) >> c.page_shift]; };
@@ -345,66 +380,73 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
     };
     auto load_keys = [&](const Where &at, CodeBlock<NG> &t) { t.k = *reinterpret_cast<const u32x4 *>(c.k_codes + at.row * 8 + 4 * lane); };
     auto load_values = [&](const Where &at, CodeBlock<NG> &t) { t.v = *reinterpret_cast<const u32x4 *>(c.v_codes + at.row * 8 + 4 * lane); };
-    // one block; done_meta, done_keys, done_values: called when that part of `cur` has been taken
-    auto process = [&](CodeBlock<NG> &cur, int blk, auto &&done_meta, auto &&done_keys, auto &&done_values) {
-      // ---- meta words: a row a lane
+    // A block's meta words, a row a lane: lanes 0-31 what concerns keys, lanes 32-63 values.
+    auto decode = [&](const CodeBlock<NG> &cur, int blk, BlockMeta<NG> &bm) {
+      const int r = lane & 31, ii = r & 3;
+      const bool part = blk * 32 + r < cur.limit && (cur.meta[0] & 0x8000u) == 0u;
+      float scale[NG], zero[NG];
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        scale[g] = part ? half_bits_to_float(cur.meta[g] & 0x7FFFu) : 1.0f;
+        zero[g] = part ? (float)((int)cur.meta[g] >> 16) : 0.0f;
+      }
+      const float top = NG == 2 && lane >= 32 ? fmaxf(scale[0], scale[NG - 1]) : scale[0], rcp = part ? __builtin_amdgcn_rcpf(top) : 0.0f;
+      const float v_log = __shfl_xor(log2_bare(top), 32, kWave) - 2.0f * (float)ii;  // (keys' lanes: of their row's values)
       bool far = false;  // a zero-point that 11 bits do not hold
-      {
-        const int r = lane & 31, ii = r & 3, at = 2 * (4 * ((r & 15) >> 2) + ii) + (r >> 4);  // the weights' order: pairs (r, r + 16)
-        const bool part = blk * 32 + r < cur.limit && (cur.meta[0] & 0x8000u) == 0u;
-        float scale[NG], zero[NG];
+      if (lane < 32) {
+        const Terms inv = split_terms(rcp), log = split_terms(part ? v_log * rcp : kNoScore);
+        const float zh = rintf(zero[0] * (1.0f / 256.0f)) * -256.0f, zl = -zero[0] - zh;
+        u32x4 *to = reinterpret_cast<u32x4 *>(&bm.start[r][0][0]);
+        to[0] = (u32x4){upper_halves(zl, zl), upper_halves(zl, zh), upper_halves(zh, zh), 0u};
+        to[1] = (u32x4){upper_halves(inv.a, inv.a), upper_halves(inv.a, inv.b), upper_halves(inv.b, inv.c), 0u};
+        to[2] = (u32x4){upper_halves(log.a, log.b), upper_halves(log.c, 0.0f), 0u, 0u};
+        to[3] = (u32x4){0u, 0u, 0u, 0u};
+        if constexpr (NG == 2) {
+          const float yh = rintf(zero[1] * (1.0f / 256.0f)) * -256.0f, yl = -zero[1] - yh;
+          *reinterpret_cast<u32x4 *>(&bm.start2[r][0]) = (u32x4){upper_halves(yl, yl), upper_halves(yl, yh), upper_halves(yh, yh), 0u};
+        }
+#pragma unroll
+        for (int g = 0; g < NG; ++g) bm.k_scale[g][r] = part || g == 0 ? scale[g] : 0.0f;
+      } else {
+        const int at = 2 * (4 * ((r & 15) >> 2) + ii) + (r >> 4);  // the weights' order: pairs (r, r + 16)
+        const float four = (float)(1 << (2 * ii));
+        bm.v_rcp[r] = rcp * four;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          scale[g] = part ? half_bits_to_float(cur.meta[g] & 0x7FFFu) : 0.0f;
-          zero[g] = part ? (float)((int)cur.meta[g] >> 16) : 0.0f;
-        }
-        if (lane < 32) {
-#pragma unroll
-          for (int g = 0; g < NG; ++g) { bm.k_scale[g][r] = scale[g]; bm.k_zero[g][r] = zero[g]; }
-        } else {
-          const float top = NG == 2 ? fmaxf(scale[0], scale[NG - 1]) : scale[0];
-          const bool any = top > 0.0f;
-          const float inv = any ? 1.0f / top : 0.0f;
-          bm.v_log[r] = any ? log2_bare(top) - 2.0f * (float)ii : -INFINITY;
-          bm.v_rcp[r] = inv * (float)(1 << (2 * ii));
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            if constexpr (NG == 2) bm.v_share[g][r] = scale[g] * inv;
-            const float hi = rintf(zero[g] * (1.0f / 2048.0f)) * 2048.0f, f = (float)(1 << (2 * ii)) * (1.0f / 64.0f);
-            bm.v_zero[0][g][at] = (uint16_t)float_to_half_bits_rne((zero[g] - hi) * f);
-            bm.v_zero[1][g][at] = (uint16_t)float_to_half_bits_rne(hi * f);
-            far = far || hi != 0.0f;
-          }
+          if constexpr (NG == 2) bm.v_share[g][r] = scale[g] * rcp;
+          const float hi = rintf(zero[g] * (1.0f / 2048.0f)) * 2048.0f, f = four * (1.0f / 64.0f);
+          bm.v_zero[0][g][at] = (uint16_t)float_to_half_bits_rne((zero[g] - hi) * f);
+          bm.v_zero[1][g][at] = (uint16_t)float_to_half_bits_rne(hi * f);
+          far = far || hi != 0.0f;
         }
       }
-      const bool any_far = __ballot(far) != 0ull;
-      wave_lds_sync();
-      done_meta();
+      bm.far = __ballot(far) != 0ull;
+    };
+    // one block; done_keys, done_values: called when that part of `cur` has been taken
+    auto process = [&](CodeBlock<NG> &cur, const BlockMeta<NG> &bm, auto &&done_keys, auto &&done_values) {
       // ---- scores and weights
       float y[QT][2][4];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const u32x2 lo = ex4(cur.k[2 * h]), hi = ex4(cur.k[2 * h + 1]);
-        u32x4 codes[NG];
-        f32x4 k_scale[NG], k_zero[NG];
-        const f32x4 v_log = *reinterpret_cast<const f32x4 *>(&bm.v_log[16 * h + 4 * q]);
+        u32x4 codes[NG], first[NG];
+        f32x4 k_scale[NG];
+        first[0] = *reinterpret_cast<const u32x4 *>(&bm.start[16 * h + n][q][0]);
         if constexpr (NG == 2) {  // a group's product takes zeros in the other group's slots
           codes[0] = (u32x4){lo[0], lo[1], 0u, 0u};
           codes[1] = (u32x4){0u, 0u, hi[0], hi[1]};
+          first[1] = *reinterpret_cast<const u32x4 *>(q == 3 ? &bm.start2[16 * h + n][0] : &sh.none[0]);
         } else {
           codes[0] = (u32x4){lo[0], lo[1], hi[0], hi[1]};
         }
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          k_scale[g] = *reinterpret_cast<const f32x4 *>(&bm.k_scale[g][16 * h + 4 * q]);
-          k_zero[g] = *reinterpret_cast<const f32x4 *>(&bm.k_zero[g][16 * h + 4 * q]);
-        }
+        for (int g = 0; g < NG; ++g) k_scale[g] = *reinterpret_cast<const f32x4 *>(&bm.k_scale[g][16 * h + 4 * q]);
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           f32x4 acc[NG];
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
-            acc[g] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            acc[g] = mfma_b16(first[g], start[t], (f32x4){0.f, 0.f, 0.f, 0.f});
             acc[g] = mfma_codes<0>(codes[g], digits[t][0], unit_exp[t], acc[g]);
             acc[g] = mfma_codes<1>(codes[g], digits[t][1], unit_exp[t], acc[g]);
             acc[g] = mfma_codes<2>(codes[g], digits[t][2], unit_exp[t], acc[g]);
@@ -412,11 +454,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float v = v_log[i];
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-              v = __builtin_fmaf(k_scale[g][i], __builtin_fmaf(-k_zero[g][i], qsum[t][g], acc[g][i]), v);
-            y[t][h][i] = v;
+            y[t][h][i] = k_scale[0][i] * acc[0][i];
+            if constexpr (NG == 2) y[t][h][i] = __builtin_fmaf(k_scale[1][i], acc[1][i], y[t][h][i]);
           }
         }
       }
@@ -425,7 +464,10 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
       const f32x4 r0 = *reinterpret_cast<const f32x4 *>(&bm.v_rcp[4 * q]), r1 = *reinterpret_cast<const f32x4 *>(&bm.v_rcp[16 + 4 * q]);
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        weigh(t, y[t], [&](float alpha) { acc_z[t] *= alpha; });
+        weigh(t, y[t], [&](float alpha) {
+          acc_z[t] *= alpha;
+          if (q == 1) start[t] = start_slots(-m[t]);
+        });
 #pragma unroll
         for (int i = 0; i < 4; ++i) l[t] = __builtin_fmaf(y[t][0][i], r0[i], __builtin_fmaf(y[t][1][i], r1[i], l[t]));
         if constexpr (NG == 2) {
@@ -443,10 +485,10 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
       // ---- values
 #pragma unroll
       for (int x = 0; x < 2; ++x)
-        if (x == 0 || any_far)
+        if (x == 0 || __builtin_amdgcn_readfirstlane(bm.far) != 0)
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
-            const u32x4 z = *reinterpret_cast<const u32x4 *>(zero_at[x][g]);
+            const u32x4 z = *reinterpret_cast<const u32x4 *>(NG == 1 || n / 8 == g ? &bm.v_zero[x][g][8 * q] : &sh.none[0]);
 #pragma unroll
             for (int t = 0; t < QT; ++t) acc_z[t] = mfma_f16(z, w[t][g], acc_z[t]);
           }
@@ -463,24 +505,42 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
         }
       }
       done_values();
-      wave_lds_sync();  // the next block's meta words overwrite this one's
     };
-    // The next block is requested while one is worked on, and its page's number one block earlier.  Many rows: each part into its own
-    // registers as soon as they are free (another set would be ten too many); few rows, bound by the stream: all of it at once.
+    // The next block is requested while one is worked on, and its page's number one block earlier.
     const int first = u0 + wk;
-    Where at = find(first, page_of(first));
-    int page = page_of(min(first + WK, n_code - 1));
-    CodeBlock<NG> buf[MANY ? 1 : 2];
-    load_meta(at, buf[0]);
-    load_keys(at, buf[0]);
-    load_values(at, buf[0]);
     if constexpr (MANY) {
-      for (int blk = first; blk < code_end; ++blk) {
-        at = find(min(blk + 1, n_code - 1), page);
-        page = page_of(min(blk + 2, n_code - 1));
-        process(buf[0], blk, [&] { load_meta(at, buf[0]); }, [&] { load_keys(at, buf[0]); }, [&] { load_values(at, buf[0]); });
+      // Every wavefront decodes one block of the next eight for all; codes go into their registers again as soon as they are free (another
+      // set would be ten registers too many).
+      CodeBlock<NG> buf, words;
+      auto ask_words = [&](int from) {
+        const int blk = min(from + wave, n_code - 1);
+        load_meta(find(blk, page_of(blk)), words);
+      };
+      ask_words(first);
+      Where at = find(first, page_of(first));
+      load_keys(at, buf);
+      load_values(at, buf);
+      int page = page_of(min(first + 1, n_code - 1));
+      for (int from = first, turn = 0; from < code_end; from += kManyWaves, turn ^= 1) {
+        decode(words, min(from + wave, n_code - 1), sh.meta[turn][wave]);
+        if (from + kManyWaves < code_end) ask_words(from + kManyWaves);
+        lds_barrier();  // (the other set was last read in front of the barrier before)
+        if (idle) continue;
+        for (int blk = from; blk < min(from + kManyWaves, code_end); ++blk) {
+          at = find(min(blk + 1, n_code - 1), page);
+          page = page_of(min(blk + 2, n_code - 1));
+          process(buf, sh.meta[turn][blk - from], [&] { load_keys(at, buf); }, [&] { load_values(at, buf); });
+        }
       }
     } else {
+      // bound by the stream: another set of registers, asked for as a whole
+      CodeBlock<NG> buf[2];
+      BlockMeta<NG> &bm = sh.meta[0][wave];
+      Where at = find(first, page_of(first));
+      int page = page_of(min(first + WK, n_code - 1));
+      load_meta(at, buf[0]);
+      load_keys(at, buf[0]);
+      load_values(at, buf[0]);
       for (int blk = first; blk < code_end; blk += 2 * WK) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -491,7 +551,10 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
           load_meta(at, buf[1 - x]);
           load_keys(at, buf[1 - x]);
           load_values(at, buf[1 - x]);
-          process(buf[x], now, [] {}, [] {}, [] {});
+          wave_lds_sync();  // the block before is done with its words
+          decode(buf[x], now, bm);
+          wave_lds_sync();
+          process(buf[x], bm, [] {}, [] {});
         }
       }
     }
@@ -574,7 +637,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) y[t][h][i] = blk * 32 + 16 * h + 4 * q + i < wide ? acc[t][i] : -INFINITY;
+          for (int i = 0; i < 4; ++i) y[t][h][i] = blk * 32 + 16 * h + 4 * q + i < wide ? acc[t][i] - m[t] : kNoScore;
       }
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
@@ -624,11 +687,12 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
       if (!a.out_rotated) wht128_output(o[t], q);
       const float all = column_sum(l[t]);
       if (all > 0.0f) {
-        const float to = m[t] + log2_bare(all) - kRaiseTo, alpha = exp2_bare(m[t] - to);
+        const float to = rintf(m[t] + log2_bare(all)) - kRaiseTo, alpha = exp2_bare(m[t] - to);
 #pragma unroll
         for (int nb = 0; nb < 8; ++nb) o[t][nb] *= alpha;
         l[t] *= alpha;
         m[t] = to;
+        limit[t] = kRaiseAt;
       }
     }
   }
@@ -664,7 +728,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) y[t][h][i] = acc[t][i] * sm2;
+          for (int i = 0; i < 4; ++i) y[t][h][i] = __builtin_fmaf(acc[t][i], sm2, -m[t]);
       }
       if (blk * 32 + 31 > low_token) {  // uniform over the wavefront: some row may not look at all of the block
 #pragma unroll
@@ -673,7 +737,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (blk * 32 + 16 * h + 4 * q + i > token[t]) y[t][h][i] = -INFINITY;
+              if (blk * 32 + 16 * h + 4 * q + i > token[t]) y[t][h][i] = kNoScore;
       }
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
@@ -733,7 +797,10 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 
   // ================= sums of the wavefronts, and out =================
 #pragma unroll
-  for (int t = 0; t < QT; ++t) l[t] = column_sum(l[t]);
+  for (int t = 0; t < QT; ++t) {
+    l[t] = column_sum(l[t]);
+    if (limit[t] < 0.0f) m[t] = kNoScore;
+  }
   auto store = [&](int row, int ch, const f32x4 &x, float top, float sum) {  // four channels of a finished or partial row
     const int token = row / R, hq = head * R + row - token * R;
     const size_t at = (size_t)(s.first + token) * a.Hq + hq;
