@@ -267,37 +267,48 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 #pragma unroll
     for (int e = 0; e < 32; ++e) x[e] *= f;
   };
-  // Weights of a tile's eight scores relative to the reference (rows 4q + i of the two halves of a block; no part: far below).  The
+  // Weights of the tiles' scores relative to the reference (rows 4q + i of the two halves of a block; no part: far below).  The
   // reference is raised, and what was summed against it rescaled (`more`: the rest of it), only when a score exceeds it by kRaiseAt.
-  auto weigh = [&](int t, float (&y)[2][4], auto &&more) {
-    float top = y[0][0];
+  auto weigh = [&](float (&y)[QT][2][4], auto &&more) {
+    float top[QT];
+    bool raise = false;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, y[h][i]);
-    if (__ballot(top > limit[t]) != 0ull) {
-      const float all = column_max(top);
-      float by = 0.0f;
-      if (all > limit[t]) {  // the four lanes of a column agree
-        const float to = rintf(m[t] + all) - kRaiseTo;
-        by = to - m[t];
-        const float alpha = limit[t] < 0.0f ? 0.0f : exp2_bare(-by);  // (there was nothing before the first score)
-#pragma unroll
-        for (int nb = 0; nb < 8; ++nb) o[t][nb] *= alpha;
-        l[t] *= alpha;
-        m[t] = to;
-        limit[t] = kRaiseAt;
-        more(alpha);
-      }
+    for (int t = 0; t < QT; ++t) {
+      top[t] = y[t][0][0];
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[h][i] -= by;
+        for (int i = 0; i < 4; ++i) top[t] = fmaxf(top[t], y[t][h][i]);
+      raise = raise || top[t] > limit[t];
+    }
+    if (__builtin_expect(__ballot(raise) != 0ull, 0)) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const float all = column_max(top[t]);
+        float by = 0.0f;
+        if (all > limit[t]) {  // the four lanes of a column agree
+          const float to = rintf(m[t] + all) - kRaiseTo;
+          by = to - m[t];
+          const float alpha = limit[t] < 0.0f ? 0.0f : exp2_bare(-by);  // (there was nothing before the first score)
+#pragma unroll
+          for (int nb = 0; nb < 8; ++nb) o[t][nb] *= alpha;
+          l[t] *= alpha;
+          m[t] = to;
+          limit[t] = kRaiseAt;
+          more(t, alpha);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[t][h][i] -= by;
+      }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int t = 0; t < QT; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[h][i] = exp2_bare(y[h][i]);
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[t][h][i] = exp2_bare(y[t][h][i]);
   };
 
   // ================= code rows =================
@@ -361,7 +372,10 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 
     if (lane < 16) reinterpret_cast<uint32_t *>(sh.none)[lane] = 0u;  // (by every wavefront for itself)
     const ExpandF4 ex4;
-    const int32_t *table = c.table + (size_t)b * c.max_pages;
+    // page numbers by scalar loads (the constant address space), whose wait stands in front of the first use: a vector load of them would
+    // be waited for where it is issued, and every other load with it
+    const auto *table = reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(
+        reinterpret_cast<uintptr_t>(c.table + (size_t)b * c.max_pages));
     auto page_of = [&](int blk) { return table[min(blk * 32, s.len - 1) >> c.page_shift]; };
     struct Where { size_t row; int limit; };  // first row of a block in the pools; rows from `limit` on (of the sequence) take no part
     auto find = [&](int blk, int page) {
@@ -425,6 +439,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
     // one block; done_keys, done_values: called when that part of `cur` has been taken
     auto process = [&](CodeBlock<NG> &cur, const BlockMeta<NG> &bm, auto &&done_keys, auto &&done_values) {
       // ---- scores and weights
+      const int far = bm.far;
       float y[QT][2][4];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -462,12 +477,12 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
       done_keys();
       u32x4 w[QT][NG];
       const f32x4 r0 = *reinterpret_cast<const f32x4 *>(&bm.v_rcp[4 * q]), r1 = *reinterpret_cast<const f32x4 *>(&bm.v_rcp[16 + 4 * q]);
+      weigh(y, [&](int t, float alpha) {
+        acc_z[t] *= alpha;
+        if (q == 1) start[t] = start_slots(-m[t]);
+      });
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        weigh(t, y[t], [&](float alpha) {
-          acc_z[t] *= alpha;
-          if (q == 1) start[t] = start_slots(-m[t]);
-        });
 #pragma unroll
         for (int i = 0; i < 4; ++i) l[t] = __builtin_fmaf(y[t][0][i], r0[i], __builtin_fmaf(y[t][1][i], r1[i], l[t]));
         if constexpr (NG == 2) {
@@ -485,7 +500,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
       // ---- values
 #pragma unroll
       for (int x = 0; x < 2; ++x)
-        if (x == 0 || __builtin_amdgcn_readfirstlane(bm.far) != 0)
+        if (x == 0 || __builtin_expect(__builtin_amdgcn_readfirstlane(far) != 0, 0))
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
             const u32x4 z = *reinterpret_cast<const u32x4 *>(NG == 1 || n / 8 == g ? &bm.v_zero[x][g][8 * q] : &sh.none[0]);
@@ -639,9 +654,9 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 #pragma unroll
           for (int i = 0; i < 4; ++i) y[t][h][i] = blk * 32 + 16 * h + 4 * q + i < wide ? acc[t][i] - m[t] : kNoScore;
       }
+      weigh(y, [](int, float) {});
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        weigh(t, y[t], [](float) {});
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           l[t] += y[t][0][i] + y[t][1][i];
@@ -739,9 +754,9 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
             for (int i = 0; i < 4; ++i)
               if (blk * 32 + 16 * h + 4 * q + i > token[t]) y[t][h][i] = kNoScore;
       }
+      weigh(y, [](int, float) {});
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        weigh(t, y[t], [](float) {});
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           l[t] += (y[t][h][0] + y[t][h][1]) + (y[t][h][2] + y[t][h][3]);
