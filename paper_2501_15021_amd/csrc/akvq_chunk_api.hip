@@ -159,6 +159,7 @@ int akvq_paged_attention(const akvq_paged *c, const akvq_chunk *rows, const void
   if (Hq <= 0 || Hq % c->Hkv != 0) return AKVQ_ERR_INVALID_ARG;
   if (Hq / c->Hkv > 8) return AKVQ_ERR_UNSUPPORTED;
   if ((int64_t)rows->n_rows * Hq >= (1ll << 31)) return AKVQ_ERR_UNSUPPORTED;
+  if ((int64_t)a.c.max_rows * (Hq / c->Hkv) > 65535ll * akvq::kPagedManyRows) return AKVQ_ERR_UNSUPPORTED;
   if (flags & ~(uint32_t)(AKVQ_Q_PREROTATED | AKVQ_OUT_ROTATED) || n_split > 1024) return AKVQ_ERR_INVALID_ARG;
   if (a.c.max_rows == 0) return AKVQ_OK;
   if (check_rows(q, q_stride, Hq) != AKVQ_OK || check_rows(k, k_stride, c->Hkv) != AKVQ_OK || check_rows(v, v_stride, c->Hkv) != AKVQ_OK ||

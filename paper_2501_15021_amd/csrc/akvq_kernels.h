@@ -416,10 +416,11 @@ struct PagedAttentionArgs {
   int q_rotated, out_rotated;
 };
 hipError_t launch_paged_attention(const PagedAttentionArgs &a, int G, hipStream_t stream);
+constexpr int kPagedManyRows = 256;  // rows (tokens x heads of a group) of a workgroup that has many; its number is a grid dimension
 // How many splits of the keys, for units (sequences x KV heads) of at most `rows` rows (tokens x heads of a group) over at most `len`
 // cached rows: so many that two workgroups a CU find work, with eight blocks of 32 keys for each of them.
 inline int paged_splits(long units, long rows, long len) {
-  const long blocks = (len + 31) / 32, tiles = rows <= 16 ? 1 : rows <= 64 ? (rows + 31) / 32 : (rows + 127) / 128;
+  const long blocks = (len + 31) / 32, tiles = rows <= 16 ? 1 : rows <= 64 ? (rows + 31) / 32 : (rows + kPagedManyRows - 1) / kPagedManyRows;
   long want = 512 / (units * tiles);
   if (want > blocks / 8) want = blocks / 8;
   if (want > 32) want = 32;
