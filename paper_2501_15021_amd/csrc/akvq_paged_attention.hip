@@ -32,6 +32,7 @@ namespace {
 constexpr int kDigits = 4;  // 3 or 4
 constexpr int kFewWaves = 4;   // of a workgroup that has few rows: they share them and deal the keys among them
 constexpr int kManyWaves = 8;  // of a workgroup that has many: each has its own, and all look at the same keys
+constexpr int kStageBlocks = 4;  // blocks of code rows that such a workgroup expands at a time, two wavefronts for each
 constexpr float kNoScore = -1.0e30f;   // score of a row that takes no part, reference of a column without scores
 constexpr float kRaiseAt = 15.0f;      // a score may exceed the reference by this (2^15 is the largest weight) ...
 constexpr float kRaiseTo = 7.0f;       // ... and then gets a reference this far below it
@@ -199,19 +200,19 @@ struct MetaWords {
   int limit;       // rows from here on (of the sequence) take no part
 };
 
-template <int NG>
-__device__ __forceinline__ void decode_meta(const MetaWords<NG> &cur, int blk, BlockMeta<NG> &bm, int lane) {
+// The common part: what scores and the denominator need.  PLACES: the factors 4^ii of values that stay in their words' places.
+template <int NG, bool PLACES, typename Meta>
+__device__ __forceinline__ void decode_meta(const MetaWords<NG> &cur, int blk, Meta &bm, int lane, float (&scale)[NG], float (&zero)[NG], float &rcp) {
   const int r = lane & 31, ii = r & 3;
   const bool part = blk * 32 + r < cur.limit && (cur.w[0] & 0x8000u) == 0u;
-  float scale[NG], zero[NG];
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     scale[g] = part ? half_bits_to_float(cur.w[g] & 0x7FFFu) : 1.0f;
     zero[g] = part ? (float)((int)cur.w[g] >> 16) : 0.0f;
   }
-  const float top = NG == 2 && lane >= 32 ? fmaxf(scale[0], scale[NG - 1]) : scale[0], rcp = part ? __builtin_amdgcn_rcpf(top) : 0.0f;
-  const float v_log = halves(log2_bare(top)).hi - 2.0f * (float)ii;  // (keys' lanes: of their row's values)
-  bool far = false;                                                  // a zero-point that 11 bits do not hold
+  const float top = NG == 2 && lane >= 32 ? fmaxf(scale[0], scale[NG - 1]) : scale[0];
+  rcp = part ? __builtin_amdgcn_rcpf(top) : 0.0f;
+  const float v_log = halves(log2_bare(top)).hi - (PLACES ? 2.0f * (float)ii : 0.0f);  // (keys' lanes: of their row's values)
   if (lane < 32) {
     const Terms inv = split_terms(rcp), log = split_terms(part ? v_log * rcp : kNoScore);
     const float zh = rintf(zero[0] * (1.0f / 256.0f)) * -256.0f, zl = -zero[0] - zh;
@@ -225,13 +226,22 @@ __device__ __forceinline__ void decode_meta(const MetaWords<NG> &cur, int blk, B
 #pragma unroll
     for (int g = 0; g < NG; ++g) bm.k_scale[g][r] = part || g == 0 ? scale[g] : 0.0f;
   } else {
+    bm.v_rcp[r] = rcp * (PLACES ? (float)(1 << (2 * ii)) : 1.0f);
+  }
+}
+// ... and what values need that stay in their words
+template <int NG>
+__device__ __forceinline__ void decode_block(const MetaWords<NG> &cur, int blk, BlockMeta<NG> &bm, int lane) {
+  float scale[NG], zero[NG], rcp;
+  decode_meta<NG, true>(cur, blk, bm, lane, scale, zero, rcp);
+  const int r = lane & 31, ii = r & 3;
+  bool far = false;  // a zero-point that 11 bits do not hold
+  if (lane >= 32) {
     const int at = 2 * (4 * ((r & 15) >> 2) + ii) + (r >> 4);  // the weights' order: pairs (r, r + 16)
-    const float four = (float)(1 << (2 * ii));
-    bm.v_rcp[r] = rcp * four;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       if constexpr (NG == 2) bm.v_share[g][r] = scale[g] * rcp;
-      const float hi = rintf(zero[g] * (1.0f / 2048.0f)) * 2048.0f, f = four * (1.0f / 64.0f);
+      const float hi = rintf(zero[g] * (1.0f / 2048.0f)) * 2048.0f, f = (float)(1 << (2 * ii)) * (1.0f / 64.0f);
       bm.v_zero[0][g][at] = (uint16_t)float_to_half_bits_rne((zero[g] - hi) * f);
       bm.v_zero[1][g][at] = (uint16_t)float_to_half_bits_rne(hi * f);
       far = far || hi != 0.0f;
@@ -239,6 +249,17 @@ __device__ __forceinline__ void decode_meta(const MetaWords<NG> &cur, int blk, B
   }
   bm.far = __ballot(far) != 0ull;
 }
+
+// A block expanded for the wavefronts of a workgroup of many rows: operands as their lanes take them.
+template <int NG>
+struct CodeBlock {
+  __attribute__((aligned(16))) uint16_t start[32][2][8];              // as in BlockMeta
+  __attribute__((aligned(16))) uint16_t start2[NG == 2 ? 32 : 1][8];
+  __attribute__((aligned(16))) float k_scale[NG][32];
+  __attribute__((aligned(16))) float v_rcp[32];                       // 1 / V scale, the larger one where there are two (no part: 0)
+  __attribute__((aligned(16))) u32x4 k[2][kWave];                     // [product][lane] codes as 4-bit floats
+  __attribute__((aligned(16))) u32x4 v[2][4][kWave];                  // [step][channel block][lane] (code - zero-point) * share of the larger scale, binary16
+};
 
 __device__ __forceinline__ void lds_barrier() {  // leaves loads from memory in flight
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -255,8 +276,10 @@ template <int G, int W, bool MANY>
 struct PagedShared;
 template <int G, int W>
 struct PagedShared<G, W, true> {
-  BlockMeta<kD / G> meta[2][kManyWaves];  // of the blocks being worked on, and the next
-  __attribute__((aligned(16))) uint16_t k[2][kStage * kD], v[2][kStage * kD];
+  union {  // code rows come first, then 16-bit rows
+    CodeBlock<kD / G> blocks[2][kStageBlocks];  // being worked on, and the next
+    struct { __attribute__((aligned(16))) uint16_t k[2][kStage * kD], v[2][kStage * kD]; };
+  };
 };
 template <int G, int W>
 struct PagedShared<G, W, false> {
@@ -337,9 +360,9 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 #pragma unroll
     for (int e = 0; e < 8 * NC; ++e) x[e] *= f;
   };
-  // Weights of a block's scores relative to the reference (no part: far below).  The reference is raised, and what was summed against it
-  // rescaled (`more`: the rest of it), only when a score exceeds it by kRaiseAt.
-  auto weigh = [&](float (&y)[NY], auto &&more) {
+  // A block's scores relative to the reference (no part: far below).  The reference is raised, and what was summed against it rescaled
+  // (`more`: the rest of it), only when a score exceeds it by kRaiseAt.
+  auto raise = [&](float (&y)[NY], auto &&more) {
     float top = y[0];
 #pragma unroll
     for (int i = 1; i < NY; ++i) top = fmaxf(top, y[i]);
@@ -360,6 +383,9 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 #pragma unroll
       for (int i = 0; i < NY; ++i) y[i] -= by;
     }
+  };
+  auto weigh = [&](float (&y)[NY]) {  // ... and their weights
+    raise(y, [](float) {});
 #pragma unroll
     for (int i = 0; i < NY; ++i) y[i] = exp2_bare(y[i]);
   };
@@ -426,11 +452,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
     for (int g = 0; g < NG; ++g) acc_z[g] = 0.0f;
 
     const ExpandF4 ex4;
-    // page numbers by scalar loads (the constant address space), whose wait stands in front of the first use: a vector load of them would
-    // be waited for where it is issued, and every other load with it
-    const auto *table = reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(
-        reinterpret_cast<uintptr_t>(c.table + (size_t)b * c.max_pages));
-    auto page_of = [&](int blk) { return table[min(blk * 32, s.len - 1) >> c.page_shift]; };
+    const int32_t *table = c.table + (size_t)b * c.max_pages;
     struct Where { size_t row; int limit; };  // first row of a block in the pools; rows from `limit` on (of the sequence) take no part
     auto find = [&](int blk, int page) {
       const bool there = page >= 0 && page < c.n_pages;
@@ -456,37 +478,26 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
         return *reinterpret_cast<const u32x4 *>(blk + 4 * lane);
       }
     };
-    // one block; done_keys, done_values: called when that part of k and v has been taken
-    auto process = [&](const u32x4 &k, const u32x4 &v, const BlockMeta<NG> &bm, auto &&done_keys, auto &&done_values) {
-      const int far = bm.far;
-      float y[NY];
-      // ---- scores
+    // scores of a block; codes(product): the row operand (W = 16: of the half that is being formed)
+    auto scores = [&](const auto &bm, float (&y)[NY], auto &&codes) {
 #pragma unroll
       for (int half = 0; half < (kWide ? 1 : 2); ++half) {
         const int row = kWide ? lane & 31 : 16 * half + n;  // of the row operands
         const u32x4 none = {0u, 0u, 0u, 0u};
-        u32x4 first[NG], codes[2];  // [product]
+        u32x4 first[NG];
         first[0] = g_lane < 2 ? *reinterpret_cast<const u32x4 *>(&bm.start[row][g_lane & 1][0]) : none;
         if constexpr (NG == 2) first[1] = g_lane == 0 ? *reinterpret_cast<const u32x4 *>(&bm.start2[row][0]) : none;
-        if constexpr (kWide) {
-          const u32x2 k0 = ex4(k[0]), k1 = ex4(k[1]), k2 = ex4(k[2]), k3 = ex4(k[3]);
-          codes[0] = (u32x4){k0[0], k0[1], k2[0], k2[1]};
-          codes[1] = (u32x4){k1[0], k1[1], k3[0], k3[1]};
-        } else {
-          const u32x2 lo = ex4(k[2 * half]), hi = ex4(k[2 * half + 1]);
-          codes[0] = (u32x4){lo[0], lo[1], NG == 2 ? 0u : hi[0], NG == 2 ? 0u : hi[1]};  // a group's product takes zeros in the other's slots
-          codes[1] = (u32x4){0u, 0u, hi[0], hi[1]};
-        }
         Acc acc[NG];
 #pragma unroll
         for (int g = 0; g < NG; ++g) acc[g] = T::bf16(first[g], start[g], T::zero());
 #pragma unroll
         for (int pr = 0; pr < (kWide ? 2 : NG); ++pr) {
           const int g = NG == 2 ? pr : 0, of = kWide ? pr : 0;
-          acc[g] = T::template codes<0>(codes[pr], digits[of][0], unit_exp, acc[g]);
-          acc[g] = T::template codes<1>(codes[pr], digits[of][1], unit_exp, acc[g]);
-          acc[g] = T::template codes<2>(codes[pr], digits[of][2], unit_exp, acc[g]);
-          if constexpr (kDigits == 4) acc[g] = T::template codes<kDigits - 1>(codes[pr], digits[of][kDigits - 1], unit_exp, acc[g]);
+          const u32x4 rows = codes(pr, half);
+          acc[g] = T::template codes<0>(rows, digits[of][0], unit_exp, acc[g]);
+          acc[g] = T::template codes<1>(rows, digits[of][1], unit_exp, acc[g]);
+          acc[g] = T::template codes<2>(rows, digits[of][2], unit_exp, acc[g]);
+          if constexpr (kDigits == 4) acc[g] = T::template codes<kDigits - 1>(rows, digits[of][kDigits - 1], unit_exp, acc[g]);
         }
 #pragma unroll
         for (int x = 0; x < (kWide ? 4 : 1); ++x) {
@@ -500,13 +511,18 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
           }
         }
       }
-      done_keys();
-      // ---- weights
-      weigh(y, [&](float alpha) {
+    };
+    auto raise_codes = [&](float (&y)[NY]) {
+      raise(y, [&](float alpha) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) acc_z[g] *= alpha;
         if (g_lane == 1) start[0] = start_slots(-m, 0x00003F80u);
       });
+    };
+    // weights of a block's scores, and their sum
+    auto weights = [&](const auto &bm, float (&y)[NY]) {
+#pragma unroll
+      for (int i = 0; i < NY; ++i) y[i] = exp2_bare(y[i]);
       float l2 = 0.0f;
 #pragma unroll
       for (int x = 0; x < NA; ++x) {
@@ -518,6 +534,10 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
         }
       }
       l += l2;
+    };
+    // values that stay in their words
+    [[maybe_unused]] auto values = [&](const u32x4 &v, const BlockMeta<NG> &bm, float (&y)[NY]) {
+      const int far = bm.far;
       u32x4 w[NG][NS];
 #pragma unroll
       for (int g = 0; g < NG; ++g)
@@ -559,34 +579,126 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
         o[j] = T::f16(vx, w[g][st], o[j]);
         o[j2] = T::f16(vy, w[g][st], o[j2]);
       }
-      done_values();
     };
-    // The next block is requested while one is worked on, and its page's number one block earlier.
     const int first = u0 + wk;
     if constexpr (MANY) {
-      // Every wavefront decodes one block of the next eight for all; codes go into their registers again as soon as they are free.
+      // The wavefronts expand the next four blocks for all, two for each block: the first its meta words and a half of its values, the
+      // second its keys and the other half.  What they need is asked for while the blocks before are worked on, and the pages'
+      // numbers (lane l: of block from + l) a round earlier.
+      const int mine = wave >> 1, part = wave & 1, h = g_lane;
+      auto ask_pages = [&](int from) { return table[min(min(from + lane, n_code - 1) * 32, s.len - 1) >> c.page_shift]; };
       MetaWords<NG> words;
-      auto ask_words = [&](int from) {
-        const int blk = min(from + wave, n_code - 1);
-        load_meta(find(blk, page_of(blk)), words);
+      u32x4 k, v_meta[2][NG];
+      u32x2 v;
+      int limit = 0;
+      auto ask = [&](int from, int pages) {
+        const Where at = find(min(from + mine, n_code - 1), __builtin_amdgcn_readlane(pages, mine));
+        const uint32_t *meta = c.v_meta + (at.row + 4 * (2 * part + h)) * NG;  // of rows 4g + i and 16 + 4g + i, g = 2 part + h
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int y = 0; y < NG; ++y) v_meta[x][y] = *reinterpret_cast<const u32x4 *>(meta + 16 * NG * x + 4 * y);
+        v = *reinterpret_cast<const u32x2 *>(c.v_codes + at.row * 8 + (16 * (2 * part + h) + n) * 4 + 2 * p);
+        if (part == 0) load_meta(at, words);
+        else k = load_codes(c.k_codes, at);
+        limit = at.limit;
       };
-      ask_words(first);
-      Where at = find(first, page_of(first));
-      u32x4 k = load_codes(c.k_codes, at), v = load_codes(c.v_codes, at);
-      int page = page_of(min(first + 1, n_code - 1));
-      for (int from = first, turn = 0; from < code_end; from += kManyWaves, turn ^= 1) {
-        decode_meta<NG>(words, min(from + wave, n_code - 1), sh.meta[turn][wave], lane);
-        if (from + kManyWaves < code_end) ask_words(from + kManyWaves);
+      auto expand = [&](int blk, CodeBlock<NG> &to) {
+        if (part == 0) {
+          float scale[NG], zero[NG], rcp;
+          decode_meta<NG, false>(words, blk, to, lane, scale, zero, rcp);
+        } else {
+          const u32x2 k0 = ex4(k[0]), k1 = ex4(k[1]), k2 = ex4(k[2]), k3 = ex4(k[3]);
+          to.k[0][lane] = (u32x4){k0[0], k0[1], k2[0], k2[1]};
+          to.k[1][lane] = (u32x4){k1[0], k1[1], k3[0], k3[1]};
+        }
+        // values: 1024 + code in place, less 1024 + zero-point: exact up to zero-points of 1024, else to 2^-11 of them; where a row has two
+        // scales, times its share of the larger one, rounded (2^-11 again): one set of weights serves both groups
+        u32x4 less[NG], share[NG];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float z[2][NG], sc[2][NG];
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              const uint32_t w = v_meta[x][NG == 2 ? i / 2 : 0][NG == 2 ? 2 * (i & 1) + g : i];
+              z[x][g] = (float)((int)w >> 16);
+              sc[x][g] = half_bits_to_float(w & 0x7FFFu);
+            }
+#pragma unroll
+          for (int g = 0; g < NG; ++g) less[g][i] = pack_f16x2(-1024.0f - z[0][g], -1024.0f - z[1][g]);
+          if constexpr (NG == 2) {
+            float inv[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) inv[x] = __builtin_amdgcn_rcpf(fmaxf(sc[x][0], sc[x][1]));
+#pragma unroll
+            for (int g = 0; g < 2; ++g) share[g][i] = pack_f16x2(sc[0][g] * inv[0], sc[1][g] * inv[1]);
+          }
+        }
+        // rows that take no part may hold anything, and 0 * NaN is no 0
+        u32x4 keep = {~0u, ~0u, ~0u, ~0u};
+        const int row = blk * 32 + 4 * (2 * part + h);
+        if (blk * 32 + 32 > limit)  // uniform
+#pragma unroll
+          for (int i = 0; i < 4; ++i) keep[i] = (row + i < limit ? 0xFFFFu : 0u) | (row + 16 + i < limit ? 0xFFFF0000u : 0u);
+#pragma unroll
+        for (int wd = 0; wd < 2; ++wd)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const int g = NG == 2 ? wd : 0;
+            u32x4 o4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t code = ((v[wd] >> (8 * x + 2 * i)) & 0x00030003u) | 0x64006400u, zi = less[g][i];
+              f16x2 val = __builtin_bit_cast(f16x2, code) + __builtin_bit_cast(f16x2, zi);
+              if constexpr (NG == 2) {
+                const uint32_t si = share[g][i];
+                val *= __builtin_bit_cast(f16x2, si);
+              }
+              o4[i] = __builtin_bit_cast(uint32_t, val) & keep[i];
+            }
+            to.v[part][2 * wd + x][lane] = o4;
+          }
+      };
+      auto block_scores = [&](const CodeBlock<NG> &bm, float (&y)[NY]) {
+        scores(bm, y, [&](int pr, int) { return bm.k[pr][lane]; });
+      };
+      auto block_values = [&](const CodeBlock<NG> &bm, float (&y)[NY]) {
+        weights(bm, y);
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+          u32x4 w;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = pack_f16x2(y[4 * st + i], y[4 * st + NY / 2 + i]);
+#pragma unroll
+          for (int j = 0; j < NB; ++j) o[j] = T::f16(bm.v[st][j][lane], w, o[j]);
+        }
+      };
+      int pages = ask_pages(first);
+      ask(first, pages);
+      pages = ask_pages(first + kStageBlocks);
+      for (int from = first, turn = 0; from < code_end; from += kStageBlocks, turn ^= 1) {
+        expand(min(from + mine, n_code - 1), sh.blocks[turn][mine]);
+        ask(from + kStageBlocks, pages);
+        pages = ask_pages(from + 2 * kStageBlocks);
         lds_barrier();  // (the other set was last read in front of the barrier before)
         if (idle) continue;
-        for (int blk = from; blk < min(from + kManyWaves, code_end); ++blk) {
-          at = find(min(blk + 1, n_code - 1), page);
-          page = page_of(min(blk + 2, n_code - 1));
-          process(k, v, sh.meta[turn][blk - from], [&] { k = load_codes(c.k_codes, at); }, [&] { v = load_codes(c.v_codes, at); });
+        const int last = min(kStageBlocks, code_end - from);
+        for (int x = 0; x < last; ++x) {
+          const CodeBlock<NG> &bm = sh.blocks[turn][x];
+          float y[NY];
+          block_scores(bm, y);
+          raise_codes(y);
+          block_values(bm, y);
         }
       }
+      lds_barrier();  // the stages of 16-bit rows lie where the blocks were
     } else {
-      // bound by the stream: another set of registers, asked for as a whole
+      // Bound by the stream: another set of registers, asked for as a whole.  Page numbers by scalar loads (the constant address space), whose
+      // wait stands in front of the first use: a vector load of a single one would be waited for where it is issued, and every other load with it.
+      const auto *pages = reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(table));
+      auto page_of = [&](int blk) { return pages[min(blk * 32, s.len - 1) >> c.page_shift]; };
       MetaWords<NG> words[2];
       u32x4 k[2], v[2];
       BlockMeta<NG> &bm = sh.meta[0][wave];
@@ -606,20 +718,35 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
           page = page_of(min(now + 2 * WK, n_code - 1));
           ask(at, 1 - x);
           wave_lds_sync();  // the block before is done with its words
-          decode_meta<NG>(words[x], now, bm, lane);
+          decode_block<NG>(words[x], now, bm, lane);
           wave_lds_sync();
-          process(k[x], v[x], bm, [] {}, [] {});
+          float y[NY];
+          scores(bm, y, [&](int pr, int half) {
+            if constexpr (kWide) {
+              const u32x2 lo = ex4(k[x][pr]), hi = ex4(k[x][2 + pr]);
+              return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+            } else {  // a group's product takes zeros in the other's slots
+              const u32x2 lo = ex4(k[x][2 * half]), hi = ex4(k[x][2 * half + 1]), none = {0u, 0u};
+              const u32x2 a0 = NG == 2 && pr == 1 ? none : lo, a1 = NG == 2 && pr == 0 ? none : hi;
+              return (u32x4){a0[0], a0[1], a1[0], a1[1]};
+            }
+          });
+          raise_codes(y);
+          weights(bm, y);
+          values(v[x], bm, y);
         }
       }
     }
     // codes were 2^-24 of themselves, zero-points 2^-6; a group's zero-points reach all of its channels
+    if constexpr (!MANY) {
 #pragma unroll
-    for (int g = 0; g < NG; ++g) acc_z[g] = -64.0f * T::column_sum(acc_z[g]);
+      for (int g = 0; g < NG; ++g) acc_z[g] = -64.0f * T::column_sum(acc_z[g]);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const float z = acc_z[NG == 2 ? j / (NB / 2) : 0];
+      for (int j = 0; j < NB; ++j) {
+        const float z = acc_z[NG == 2 ? j / (NB / 2) : 0];
 #pragma unroll
-      for (int i = 0; i < (kWide ? 16 : 4); ++i) o[j][i] = __builtin_fmaf(o[j][i], 16777216.0f, z);
+        for (int i = 0; i < (kWide ? 16 : 4); ++i) o[j][i] = __builtin_fmaf(o[j][i], 16777216.0f, z);
+      }
     }
   }
 
@@ -691,7 +818,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
       score16(y, key, [&](u32x4 k, int at, Acc acc) { return T::bf16(k, q_hi[at], T::bf16(k, q_lo[at], acc)); });
 #pragma unroll
       for (int i = 0; i < NY; ++i) y[i] = blk * 32 + row_of(i) < wide ? y[i] - m : kNoScore;
-      weigh(y, [](float) {});
+      weigh(y);
 #pragma unroll
       for (int i = 0; i < NY; ++i) l += y[i];
 #pragma unroll
@@ -779,7 +906,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
         for (int i = 0; i < NY; ++i)
           if (blk * 32 + row_of(i) > my_token) y[i] = kNoScore;
       }
-      weigh(y, [](float) {});
+      weigh(y);
       float l2 = 0.0f;
 #pragma unroll
       for (int i = 0; i < NY; i += 2) {
