@@ -54,6 +54,11 @@ __device__ __forceinline__ Halves halves(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return {__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
+// ... of lanes l and l ^ 16, the one whose bit 4 is clear first.
+__device__ __forceinline__ Halves neighbours(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return {__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
 __device__ __forceinline__ float halves_max(float v) {
   const Halves h = halves(v);
   return fmaxf(h.lo, h.hi);
@@ -110,8 +115,14 @@ struct Tile<16> {
     const i32x8 b = {(int)d[0], (int)d[1], (int)d[2], (int)d[3], (int)d[4], (int)d[5], 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 2, 0, 127, DIGIT, (int)scale);
   }
-  static __device__ __forceinline__ float column_max(float v) { return halves_max(fmaxf(v, __shfl_xor(v, 16, kWave))); }
-  static __device__ __forceinline__ float column_sum(float v) { return halves_sum(v + __shfl_xor(v, 16, kWave)); }
+  static __device__ __forceinline__ float column_max(float v) {
+    const Halves h = neighbours(v);
+    return halves_max(fmaxf(h.lo, h.hi));
+  }
+  static __device__ __forceinline__ float column_sum(float v) {
+    const Halves h = neighbours(v);
+    return halves_sum(h.lo + h.hi);
+  }
   static __device__ __forceinline__ int row(int a, int g) { return 16 * a + 4 * g; }
   static __device__ __forceinline__ int channel(int j, int, int g) { return 16 * j + 4 * g; }
 };
@@ -126,22 +137,14 @@ __device__ __forceinline__ void butterflies(float (&x)[N], int s) {
       x[e + s] = a - b;
     }
 }
-// one level across lanes: lane ^ 32 (exact products, one rounding), lane ^ 16
-template <int N>
-__device__ __forceinline__ void butterflies32(float (&x)[N], int lane) {
-  const float sign = lane < 32 ? 1.0f : -1.0f;
+// one level across lanes, lane ^ 32 or lane ^ 16: exact products, one rounding
+template <int ACROSS, int N>
+__device__ __forceinline__ void butterflies_across(float (&x)[N], int lane) {
+  const float sign = (lane & ACROSS) ? -1.0f : 1.0f;
 #pragma unroll
   for (int e = 0; e < N; ++e) {
-    const Halves h = halves(x[e]);
+    const Halves h = ACROSS == 32 ? halves(x[e]) : neighbours(x[e]);
     x[e] = __builtin_fmaf(sign, h.hi, h.lo);
-  }
-}
-template <int N>
-__device__ __forceinline__ void butterflies16(float (&x)[N], int lane) {
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const float p = __shfl_xor(x[e], 16, kWave);
-    x[e] = (lane & 16) ? p - x[e] : x[e] + p;
   }
 }
 // 128-point transforms without their factor, of a query column and of an output column in the layouts of Tile
@@ -149,8 +152,8 @@ template <int W, int N>
 __device__ __forceinline__ void wht128_query(float (&x)[N], int lane) {
 #pragma unroll
   for (int s = 1; s < 8; s *= 2) butterflies(x, s);
-  if constexpr (W == 16) butterflies16(x, lane);
-  butterflies32(x, lane);
+  if constexpr (W == 16) butterflies_across<16>(x, lane);
+  butterflies_across<32>(x, lane);
 #pragma unroll
   for (int s = 8; s < N; s *= 2) butterflies(x, s);
 }
@@ -158,8 +161,8 @@ template <int W, int N>
 __device__ __forceinline__ void wht128_output(float (&x)[N], int lane) {
   butterflies(x, 1);
   butterflies(x, 2);
-  if constexpr (W == 16) butterflies16(x, lane);
-  butterflies32(x, lane);
+  if constexpr (W == 16) butterflies_across<16>(x, lane);
+  butterflies_across<32>(x, lane);
 #pragma unroll
   for (int s = 4; s < N; s *= 2) butterflies(x, s);
 }
@@ -283,9 +286,13 @@ struct PagedShared<G, W, true> {
 };
 template <int G, int W>
 struct PagedShared<G, W, false> {
-  BlockMeta<kD / G> meta[1][kFewWaves];
-  __attribute__((aligned(16))) uint16_t v[kFewWaves][32 * kD];
-  __attribute__((aligned(16))) float o[kFewWaves][W][kD + 4];
+  union {  // the sums of the wavefronts come last
+    struct {
+      BlockMeta<kD / G> meta[1][kFewWaves];
+      __attribute__((aligned(16))) uint16_t v[kFewWaves][32 * kD];
+    };
+    __attribute__((aligned(16))) float o[kFewWaves][W][kD + 4];
+  };
   float m[kFewWaves][W], l[kFewWaves][W];
 };
 
@@ -312,8 +319,11 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 
   // ---- the keys of this workgroup: blocks of 32 code rows, of 32 overlay slots, of 32 chunk rows, dealt to the splits as one list
   const int32_t *sidx = c.sal_idx + (size_t)unit * c.S_cap;
+  const int entry = sidx[lane];                                 // (S_cap >= 64: asked for together with the count)
   int wide = min(max(c.sal_cnt[unit], 0), c.S_cap);             // overlay slots of cached rows (the list may be final for new rows, too)
-  {
+  if (wide <= kWave) {
+    wide = __popcll(__ballot(lane < wide && entry < s.len));
+  } else {
     int base = 0, span = wide;                                  // entries below s.len: an ascending list, sampled
     while (span > 0) {
       const int step = (span + 63) >> 6;
@@ -390,63 +400,29 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
     for (int i = 0; i < NY; ++i) y[i] = exp2_bare(y[i]);
   };
 
+  const int code_end = min(u1, n_code), wide_begin = max(u0 - n_code, 0), wide_end = min(u1 - n_code, n_wide);
+  // against 16-bit rows the query is two bfloat16 terms, 16 bits; where registers allow, made together with the digits
+  constexpr bool kKeep16 = W == 16;
+  u32x4 q_hi[NC], q_lo[NC];
+  const int wide_first = wide_begin + (MANY ? 0 : WK - 1 - wk);  // (the last wavefronts have the fewest code rows)
+  auto split_query = [&](const float (&x)[8 * NC]) {
+#pragma unroll
+    for (int k = 0; k < NC; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x0 = x[8 * k + 2 * i], x1 = x[8 * k + 2 * i + 1];
+        const uint32_t hi = pack_bf16x2(x0, x1);
+        q_hi[k][i] = hi;
+        q_lo[k][i] = pack_bf16x2(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xFFFF0000u));
+      }
+  };
+
   // ================= code rows =================
-  const int code_end = min(u1, n_code);
   if (MANY ? u0 < code_end : u0 + wk < code_end) {
     // Query digits.  A lane's inner slots of a product are what ExpandF4 makes of two code words: slot v is word v / 16, field f = 2 (v % 8) +
     // (v / 8) % 2, channel 32 (2w + f / 8) + 8c + f % 8 of the words' chunk c, where W = 32: product 0 takes words w = 0 of chunks
     // c = h and 2 + h, product 1 their words w = 1 (a group each where there are two); W = 16: one product, words 0 and 1 of chunk q.
     constexpr int NP = kWide ? 2 : 1;
-    u32x6 digits[NP][kDigits];
-    uint32_t unit_exp;
-    u32x4 start[NG];  // column operands of the first product: terms of the query's sum, of minus the reference, ones
-    auto start_slots = [&](float v, uint32_t ones) {
-      const Terms x = split_terms(v);
-      return (u32x4){upper_halves(x.a, x.b), upper_halves(x.c, x.a), upper_halves(x.b, g_lane == 1 ? x.a : x.c), ones};
-    };
-    {
-      float x[8 * NC], mx = 0.0f;
-      rotated(x);
-#pragma unroll
-      for (int e = 0; e < 8 * NC; ++e) mx = fmaxf(mx, fabsf(x[e]));
-      mx = T::column_max(mx);
-      // integers of up to 5 kDigits - 1 bits and a sign in units of a power of two U, |x| < 2^(5 kDigits - 1) U
-      const uint32_t e_biased = min(max(__float_as_uint(mx) >> 23, 20u), 250u);  // mx < 2^(e_biased - 126)
-      const float unit_inv = __uint_as_float((252u + 5u * kDigits - e_biased) << 23), u = 1.0f / unit_inv;
-      float sum[2] = {0.0f, 0.0f};
-      constexpr int kLower = kDigits == 4 ? 16 * (1 + 32 + 1024) : 16 * (1 + 32);  // lower digits offset to 0 .. 31
-      int v[8 * NC];
-#pragma unroll
-      for (int e = 0; e < 8 * NC; ++e) {
-        const float nf = rintf(x[e] * unit_inv);
-        sum[e / (4 * NC)] += nf * u;  // (the upper half of a lane's channels is the second group)
-        v[e] = (int)nf + kLower;
-      }
-#pragma unroll
-      for (int pr = 0; pr < NP; ++pr)
-#pragma unroll
-        for (int d = 0; d < kDigits; ++d) {
-          f32x16 dig[2];  // even and odd slots, as the packing conversion takes them
-#pragma unroll
-          for (int slot = 0; slot < 32; ++slot) {
-            const int f = 2 * (slot & 7) + ((slot >> 3) & 1), word = slot >> 4;
-            // W = 32: x[16 m + 8 s + i] with m = 2 pr + f / 8, s = word; W = 16: x[8 m + i] with m = 2 word + f / 8
-            const int e = kWide ? 16 * (2 * pr + (f >> 3)) + 8 * word + (f & 7) : 8 * (2 * word + (f >> 3)) + (f & 7);
-            dig[slot & 1][slot >> 1] = 0.125f * (float)(d == kDigits - 1 ? v[e] >> (5 * d) : ((v[e] >> (5 * d)) & 31) - 16);
-          }
-          digits[pr][d] = __builtin_bit_cast(u32x6, __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(dig[0], dig[1], 1.0f));
-          // The conversion reads its operands while it already writes: they are kept past it, so that the result gets registers of its own.
-          // (And one digit after the other: all of them at once take 128 registers.)
-          asm volatile("" ::"v"(dig[0]), "v"(dig[1]), "v"(digits[pr][d]) : "memory");
-        }
-      const float s0 = T::column_sum(NG == 2 ? sum[0] : sum[0] + sum[1]);
-      start[0] = start_slots(g_lane == 0 ? s0 : 0.0f, g_lane == 0 ? 0x3F803F80u : g_lane == 1 ? 0x00003F80u : 0u);
-      if constexpr (NG == 2) {
-        const float s1 = T::column_sum(sum[1]);
-        start[1] = start_slots(g_lane == 0 ? s1 : 0.0f, 0u);
-      }
-      unit_exp = (e_biased + 6u - 5u * kDigits) * 0x01010101u + 0x0F0A0500u;  // a byte a digit: each 32 times the one below
-    }
     float acc_z[NG];  // this lane's share of the sums of weight * zero-point / 64
 #pragma unroll
     for (int g = 0; g < NG; ++g) acc_z[g] = 0.0f;
@@ -478,6 +454,80 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
         return *reinterpret_cast<const u32x4 *>(blk + 4 * lane);
       }
     };
+    const int first = u0 + wk;
+    // few rows, bound by the stream: two sets of registers, each asked for as a whole, the first in front of the query's preparation.  Page numbers
+    // by scalar loads (the constant address space), whose wait stands in front of the first use: a vector load of a single one would be
+    // waited for where it is issued, and every other load with it.
+    const auto *page_at = reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(table));
+    auto page_of = [&](int blk) { return page_at[min(blk * 32, s.len - 1) >> c.page_shift]; };
+    MetaWords<NG> few_words[2];
+    u32x4 few_k[2], few_v[2];
+    auto ask_few = [&](const Where &at, int x) {
+      load_meta(at, few_words[x]);
+      few_k[x] = load_codes(c.k_codes, at);
+      few_v[x] = load_codes(c.v_codes, at);
+    };
+    int few_page = 0;
+    if constexpr (!MANY) {
+      const int page = page_of(first);
+      few_page = page_of(min(first + WK, n_code - 1));
+      ask_few(find(first, page), 0);
+    }
+    u32x6 digits[NP][kDigits];
+    uint32_t unit_exp;
+    u32x4 start[NG];  // column operands of the first product: terms of the query's sum, of minus the reference, ones
+    auto start_slots = [&](float v, uint32_t ones) {
+      const Terms x = split_terms(v);
+      return (u32x4){upper_halves(x.a, x.b), upper_halves(x.c, x.a), upper_halves(x.b, g_lane == 1 ? x.a : x.c), ones};
+    };
+    {
+      float x[8 * NC], mx = 0.0f;
+      rotated(x);
+      if constexpr (kKeep16) split_query(x);
+#pragma unroll
+      for (int e = 0; e < 8 * NC; ++e) mx = fmaxf(mx, fabsf(x[e]));
+      mx = T::column_max(mx);
+      // integers of up to 5 kDigits - 1 bits and a sign in units of a power of two U, |x| < 2^(5 kDigits - 1) U
+      const uint32_t e_biased = min(max(__float_as_uint(mx) >> 23, 20u), 250u);  // mx < 2^(e_biased - 126)
+      const float unit_inv = __uint_as_float((252u + 5u * kDigits - e_biased) << 23), u = 1.0f / unit_inv;
+      float sum[2] = {0.0f, 0.0f};
+      // digit k of n is the signed five-bit field k of ((n + b) ^ b), b = 16 in every lower digit
+      constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer in the low bits
+      constexpr int kHalf = kDigits == 4 ? 16 * (1 + 32 + 1024) : 16 * (1 + 32);
+      int v[8 * NC];
+#pragma unroll
+      for (int e = 0; e < 8 * NC; ++e) {
+        const float t = __builtin_fmaf(x[e], unit_inv, kMagic);
+        sum[e / (4 * NC)] += t - kMagic;  // (the upper half of a lane's channels is the second group)
+        v[e] = (__float_as_int(t) + (kHalf - 0x4B400000)) ^ kHalf;
+      }
+#pragma unroll
+      for (int pr = 0; pr < NP; ++pr)
+#pragma unroll
+        for (int d = 0; d < kDigits; ++d) {
+          f32x16 dig[2];  // even and odd slots, as the packing conversion takes them
+#pragma unroll
+          for (int slot = 0; slot < 32; ++slot) {
+            const int f = 2 * (slot & 7) + ((slot >> 3) & 1), word = slot >> 4;
+            // W = 32: x[16 m + 8 s + i] with m = 2 pr + f / 8, s = word; W = 16: x[8 m + i] with m = 2 word + f / 8
+            const int e = kWide ? 16 * (2 * pr + (f >> 3)) + 8 * word + (f & 7) : 8 * (2 * word + (f >> 3)) + (f & 7);
+            dig[slot & 1][slot >> 1] = (float)(d == kDigits - 1 ? v[e] >> (5 * d) : (int)__builtin_amdgcn_sbfe(v[e], 5 * d, 5));
+          }
+          digits[pr][d] = __builtin_bit_cast(u32x6, __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(dig[0], dig[1], 8.0f));
+          // The conversion reads its operands while it already writes: they are kept past it, so that the result gets registers of its own.
+          // (And one digit after the other: all of them at once take 128 registers.)
+          asm volatile("" ::"v"(dig[0]), "v"(dig[1]), "v"(digits[pr][d]) : "memory");
+        }
+      sum[0] *= u;
+      sum[1] *= u;
+      const float s0 = T::column_sum(NG == 2 ? sum[0] : sum[0] + sum[1]);
+      start[0] = start_slots(g_lane == 0 ? s0 : 0.0f, g_lane == 0 ? 0x3F803F80u : g_lane == 1 ? 0x00003F80u : 0u);
+      if constexpr (NG == 2) {
+        const float s1 = T::column_sum(sum[1]);
+        start[1] = start_slots(g_lane == 0 ? s1 : 0.0f, 0u);
+      }
+      unit_exp = (e_biased + 6u - 5u * kDigits) * 0x01010101u + 0x0F0A0500u;  // a byte a digit: each 32 times the one below
+    }
     // scores of a block; codes(product): the row operand (W = 16: of the half that is being formed)
     auto scores = [&](const auto &bm, float (&y)[NY], auto &&codes) {
 #pragma unroll
@@ -580,7 +630,6 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
         o[j2] = T::f16(vy, w[g][st], o[j2]);
       }
     };
-    const int first = u0 + wk;
     if constexpr (MANY) {
       // The wavefronts expand the next four blocks for all, two for each block: the first its meta words and a half of its values, the
       // second its keys and the other half.  What they need is asked for while the blocks before are worked on, and the pages'
@@ -695,45 +744,32 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
       }
       lds_barrier();  // the stages of 16-bit rows lie where the blocks were
     } else {
-      // Bound by the stream: another set of registers, asked for as a whole.  Page numbers by scalar loads (the constant address space), whose
-      // wait stands in front of the first use: a vector load of a single one would be waited for where it is issued, and every other load with it.
-      const auto *pages = reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(table));
-      auto page_of = [&](int blk) { return pages[min(blk * 32, s.len - 1) >> c.page_shift]; };
-      MetaWords<NG> words[2];
-      u32x4 k[2], v[2];
       BlockMeta<NG> &bm = sh.meta[0][wave];
-      auto ask = [&](const Where &at, int x) {
-        load_meta(at, words[x]);
-        k[x] = load_codes(c.k_codes, at);
-        v[x] = load_codes(c.v_codes, at);
-      };
-      ask(find(first, page_of(first)), 0);
-      int page = page_of(min(first + WK, n_code - 1));
       for (int blk = first; blk < code_end; blk += 2 * WK) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int now = blk + x * WK;
           if (now >= code_end) break;
-          const Where at = find(min(now + WK, n_code - 1), page);
-          page = page_of(min(now + 2 * WK, n_code - 1));
-          ask(at, 1 - x);
+          const Where at = find(min(now + WK, n_code - 1), few_page);
+          few_page = page_of(min(now + 2 * WK, n_code - 1));
+          ask_few(at, 1 - x);
           wave_lds_sync();  // the block before is done with its words
-          decode_block<NG>(words[x], now, bm, lane);
+          decode_block<NG>(few_words[x], now, bm, lane);
           wave_lds_sync();
           float y[NY];
           scores(bm, y, [&](int pr, int half) {
             if constexpr (kWide) {
-              const u32x2 lo = ex4(k[x][pr]), hi = ex4(k[x][2 + pr]);
+              const u32x2 lo = ex4(few_k[x][pr]), hi = ex4(few_k[x][2 + pr]);
               return (u32x4){lo[0], lo[1], hi[0], hi[1]};
             } else {  // a group's product takes zeros in the other's slots
-              const u32x2 lo = ex4(k[x][2 * half]), hi = ex4(k[x][2 * half + 1]), none = {0u, 0u};
+              const u32x2 lo = ex4(few_k[x][2 * half]), hi = ex4(few_k[x][2 * half + 1]), none = {0u, 0u};
               const u32x2 a0 = NG == 2 && pr == 1 ? none : lo, a1 = NG == 2 && pr == 0 ? none : hi;
               return (u32x4){a0[0], a0[1], a1[0], a1[1]};
             }
           });
           raise_codes(y);
           weights(bm, y);
-          values(v[x], bm, y);
+          values(few_v[x], bm, y);
         }
       }
     }
@@ -795,21 +831,11 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
   auto row_of = [&](int i) { return T::row(i >> 2, g_lane) + (i & 3); };  // of y[i], in its block
 
   // ================= 16-bit rows of the cache =================
-  const int wide_begin = max(u0 - n_code, 0), wide_end = min(u1 - n_code, n_wide);
   if (wide_begin < wide_end) {
-    u32x4 q_hi[NC], q_lo[NC];  // two bfloat16 terms: 16 bits of the query
-    {
+    if (!kKeep16 || u0 + wk >= code_end) {
       float x[8 * NC];
       rotated(x);
-#pragma unroll
-      for (int k = 0; k < NC; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x0 = x[8 * k + 2 * i], x1 = x[8 * k + 2 * i + 1];
-          const uint32_t hi = pack_bf16x2(x0, x1);
-          q_hi[k][i] = hi;
-          q_lo[k][i] = pack_bf16x2(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xFFFF0000u));
-        }
+      split_query(x);
     }
     const uint16_t *ks = c.k_sal + (size_t)unit * c.S_cap * kD, *vs = c.v_sal + (size_t)unit * c.S_cap * kD;
     // one block of 32 slots; value(nb, g): the 16 bytes of the tile for channels 16nb + n, rows 4g + i and 16 + 4g + i
@@ -859,14 +885,14 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
                               [&](int nb, int g) { return *reinterpret_cast<const u32x4 *>(&sh.v[buf][x * 4096 + nb * 512 + 8 * (16 * g + n)]); });
              });
     } else {
-      for (int blk = wide_begin + wk; blk < wide_end; blk += WK)
+      for (int blk = wide_first; blk < wide_end; blk += WK)
         wide_block(blk, [&](int half, int k) { return *reinterpret_cast<const u32x4 *>(ks + (size_t)(blk * 32 + 16 * half + col) * kD + kD / NC * k + 8 * g_lane); },
                    [&](int nb, int g) { return *reinterpret_cast<const u32x4 *>(vs + (size_t)blk * 4096 + nb * 512 + 8 * (16 * g + n)); });
     }
   }
   // The cached rows' share is rotated back (H is its own inverse), and the chunk's rows join it.  Their weights are relative to the
   // sum so far: the reference of the code rows holds V scales as well.
-  if (!idle && u0 + wk < n_code + n_wide) {
+  if (!idle && (u0 + wk < code_end || wide_first < wide_end)) {
     constexpr int NO = kWide ? 16 : 4;
     if (!a.out_rotated) {
       float x[NB * NO];
@@ -954,7 +980,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
              });
     } else {
       uint16_t *vt = sh.v[wave];
-      for (int blk = self_begin + wk; blk < min(self_end, my_end); blk += WK) {
+      for (int blk = self_begin + WK - 1 - wk; blk < min(self_end, my_end); blk += WK) {
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           const int row = 4 * x + (lane >> 4);
@@ -994,6 +1020,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 #pragma unroll
         for (int x = 0; x < (kWide ? 4 : 1); ++x) store(row0 + col, T::channel(j, x, g_lane), part_of(j, x), m, l);
   } else {
+    __syncthreads();  // (the sums lie where other wavefronts may still read)
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
