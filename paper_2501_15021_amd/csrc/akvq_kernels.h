@@ -418,11 +418,12 @@ struct PagedAttentionArgs {
 hipError_t launch_paged_attention(const PagedAttentionArgs &a, int G, hipStream_t stream);
 constexpr int kPagedManyRows = 256;  // rows (tokens x heads of a group) of a workgroup that has many; its number is a grid dimension
 // How many splits of the keys, for units (sequences x KV heads) of at most `rows` rows (tokens x heads of a group) over at most `len`
-// cached rows: so many that two workgroups a CU find work, with eight blocks of 32 keys for each of them.
+// cached rows: so many that as many workgroups as fit on a CU find work (three of up to 16 rows, else two; more than that and the merge
+// costs what the balance gains), with four blocks of 32 keys or more for each of them.
 inline int paged_splits(long units, long rows, long len) {
   const long blocks = (len + 31) / 32, tiles = rows <= 16 ? 1 : rows <= 64 ? (rows + 31) / 32 : (rows + kPagedManyRows - 1) / kPagedManyRows;
-  long want = 512 / (units * tiles);
-  if (want > blocks / 8) want = blocks / 8;
+  long want = (rows <= 16 ? 768 : 512) / (units * tiles);
+  if (want > blocks / 4) want = blocks / 4;
   if (want > 32) want = 32;
   return (int)(want < 1 ? 1 : want);
 }

@@ -127,6 +127,9 @@ struct Tile<16> {
   static __device__ __forceinline__ int channel(int j, int, int g) { return 16 * j + 4 * g; }
 };
 
+template <int CTRL>
+struct Dpp { static constexpr int value = CTRL; };
+
 template <int N>
 __device__ __forceinline__ void butterflies(float (&x)[N], int s) {
 #pragma unroll
@@ -147,16 +150,7 @@ __device__ __forceinline__ void butterflies_across(float (&x)[N], int lane) {
     x[e] = __builtin_fmaf(sign, h.hi, h.lo);
   }
 }
-// 128-point transforms without their factor, of a query column and of an output column in the layouts of Tile
-template <int W, int N>
-__device__ __forceinline__ void wht128_query(float (&x)[N], int lane) {
-#pragma unroll
-  for (int s = 1; s < 8; s *= 2) butterflies(x, s);
-  if constexpr (W == 16) butterflies_across<16>(x, lane);
-  butterflies_across<32>(x, lane);
-#pragma unroll
-  for (int s = 8; s < N; s *= 2) butterflies(x, s);
-}
+// 128-point transform without its factor of an output column in the layout of Tile
 template <int W, int N>
 __device__ __forceinline__ void wht128_output(float (&x)[N], int lane) {
   butterflies(x, 1);
@@ -165,6 +159,48 @@ __device__ __forceinline__ void wht128_output(float (&x)[N], int lane) {
   butterflies_across<32>(x, lane);
 #pragma unroll
   for (int s = 4; s < N; s *= 2) butterflies(x, s);
+}
+// The transform of query columns as they are loaded, x[8k + i] = channel i of chunk k: by products with the matrix's signs, which binary16
+// holds exactly (a hundred instructions; butterflies between lanes and registers take three times as many).  Row r of an operand is
+// output channel e(r), inner slot j of lane group g channel c(g, j) of a chunk; the sign is the parity of e & c, so what depends on the chunk's
+// number alone is left to a four-point transform of the results.
+__device__ __forceinline__ u32x4 sign_row(int r, uint32_t base, uint32_t upper) {  // parities with r % 4 (slots j % 4), and of j / 4 = 1
+  const uint32_t w0 = 0x3C003C00u ^ base ^ ((r & 1) ? 0x80000000u : 0u), w1 = 0x3C003C00u ^ base ^ ((r & 1) ? 0x80000000u : 0u) ^ ((r & 2) ? 0x80008000u : 0u);
+  return (u32x4){w0, w1, w0 ^ upper, w1 ^ upper};
+}
+constexpr uint32_t kMinus = 0x80008000u;
+__device__ __forceinline__ void rotate_query_columns(const u32x4 (&raw)[4], float (&x)[32], int lane) {  // W = 16
+  // e = 32m + 8 (r / 4) + 4 hi + r % 4, c = 32k + 8g + j
+  const int r = lane & 15, g = lane >> 4;
+  const uint32_t base = (__popc((r >> 2) & g) & 1) ? kMinus : 0u;
+#pragma unroll
+  for (int hi = 0; hi < 2; ++hi) {
+    const u32x4 a = sign_row(r, base, hi ? kMinus : 0u);
+    f32x4 t[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) t[k] = Tile<16>::f16(a, raw[k], Tile<16>::zero());
+    const f32x4 s0 = t[0] + t[1], d0 = t[0] - t[1], s1 = t[2] + t[3], d1 = t[2] - t[3];
+    const f32x4 y[4] = {s0 + s1, d0 + d1, s0 - s1, d0 - d1};
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[8 * m + 4 * hi + i] = y[m][i];
+  }
+}
+__device__ __forceinline__ void rotate_query_columns(const u32x4 (&raw)[8], float (&x)[64], int lane) {  // W = 32
+  // row r = 8a + 4h + i of an operand: e = 32b + 16 (a / 2) + 8h + 4 (a % 2) + i; c = 16k + 8g + j
+  const int r = lane & 31, g = lane >> 5;
+  const uint32_t base = ((r >> 2) & g & 1) ? kMinus : 0u, upper = ((r >> 3) & 1) ? kMinus : 0u;
+  const u32x4 a0 = sign_row(r, base, upper), a1 = sign_row(r, base ^ (((r >> 4) & 1) ? kMinus : 0u), upper);
+  f32x16 t[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) t[k] = Tile<32>::f16(a1, raw[2 * k + 1], Tile<32>::f16(a0, raw[2 * k], Tile<32>::zero()));
+  const f32x16 s0 = t[0] + t[1], d0 = t[0] - t[1], s1 = t[2] + t[3], d1 = t[2] - t[3];
+  const f32x16 y[4] = {s0 + s1, d0 + d1, s0 - s1, d0 - d1};
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[16 * b + e] = y[b][e];
 }
 
 // A float as three bfloat16 terms (its 24 bits), in the upper halves.
@@ -284,20 +320,34 @@ struct PagedShared<G, W, true> {
     struct { __attribute__((aligned(16))) uint16_t k[2][kStage * kD], v[2][kStage * kD]; };
   };
 };
-template <int G, int W>
-struct PagedShared<G, W, false> {
+template <int G>
+struct PagedShared<G, 16, false> {
+  union {  // of every wavefront its own: a block's meta words and the next one's, then its sums
+    BlockMeta<kD / G> meta[2];
+    __attribute__((aligned(16))) float o[16][kD + 4];
+  } own[kFewWaves];
+  union {
+    uint32_t digits[1][kDigits][6][kWave];
+    __attribute__((aligned(16))) float self[16][kD + 4];  // sums over the chunk's rows
+  };
+  __attribute__((aligned(16))) uint16_t v[1][32 * kD];    // (sixteen rows of a unit are of one block of the chunk)
+  float m[kFewWaves + 1][16], l[kFewWaves + 1][16];
+};
+template <int G>
+struct PagedShared<G, 32, false> {
   union {  // the sums of the wavefronts come last
     struct {
-      BlockMeta<kD / G> meta[1][kFewWaves];
+      struct { BlockMeta<kD / G> meta[2]; } own[kFewWaves];
       __attribute__((aligned(16))) uint16_t v[kFewWaves][32 * kD];
+      uint32_t digits[2][kDigits][6][kWave];
     };
-    __attribute__((aligned(16))) float o[kFewWaves][W][kD + 4];
+    __attribute__((aligned(16))) float o[kFewWaves][32][kD + 4];
   };
-  float m[kFewWaves][W], l[kFewWaves][W];
+  float m[kFewWaves][32], l[kFewWaves][32];
 };
 
 template <int G, int W, bool MANY>
-__global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged_attention_kernel(PagedAttentionArgs a) {
+__global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 : 2) void paged_attention_kernel(PagedAttentionArgs a) {
   typedef Tile<W> T;
   typedef typename T::Acc Acc;
   constexpr int NG = kD / G, NW = MANY ? kManyWaves : kFewWaves, WK = MANY ? 1 : NW, kWide = W == 32;
@@ -336,8 +386,14 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
   }
   const int last_row = min(wg_row + (MANY ? NW : 1) * W, rows) - 1;
   const int n_code = (s.len + 31) >> 5, n_wide = (wide + 31) >> 5, n_self = last_row / R / 32 + 1;
-  int u0, u1;
-  decode_split_range(n_code + n_wide + n_self, a.n_split, split, u0, u1);
+  // equal runs of the list, of a workgroup (many rows) or of a wavefront (few): a block of 16-bit rows counts as two of code rows
+  const int parts = a.n_split * WK, wide_at = n_code, self_at = n_code + 2 * n_wide;
+  const int run = (self_at + 2 * n_self) / parts, longer = self_at + 2 * n_self - run * parts;  // the first runs are longer by one
+  auto run_start = [&](int part) { return run * part + min(part, longer); };
+  const int run_begin = run_start(split * WK + wk), run_end = run_start(split * WK + wk + 1), group_begin = run_start(split * WK);
+  const int code_begin = min(run_begin, n_code), code_end = min(run_end, n_code);
+  const int wide_begin = min((max(run_begin - wide_at, 0) + 1) / 2, n_wide), wide_end = min((max(run_end - wide_at, 0) + 1) / 2, n_wide);
+  const int self_begin = min((max(run_begin - self_at, 0) + 1) / 2, n_self), self_end = min((max(run_end - self_at, 0) + 1) / 2, n_self);
 
   Acc o[NB];
 #pragma unroll
@@ -355,17 +411,18 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
   auto rotated = [&](float (&x)[8 * NC]) {
     u32x4 raw[NC];
     load_query(raw);
-#pragma unroll
-    for (int k = 0; k < NC; ++k)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        x[8 * k + 2 * w] = half_bits_to_float(raw[k][w] & 0xFFFFu);
-        x[8 * k + 2 * w + 1] = half_bits_to_float(raw[k][w] >> 16);
-      }
     float f = sm2;
     if (!a.q_rotated) {
-      wht128_query<W>(x, lane);
+      rotate_query_columns(raw, x, lane);
       f *= inv_sqrt128();
+    } else {
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          x[8 * k + 2 * w] = half_bits_to_float(raw[k][w] & 0xFFFFu);
+          x[8 * k + 2 * w + 1] = half_bits_to_float(raw[k][w] >> 16);
+        }
     }
 #pragma unroll
     for (int e = 0; e < 8 * NC; ++e) x[e] *= f;
@@ -400,11 +457,10 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
     for (int i = 0; i < NY; ++i) y[i] = exp2_bare(y[i]);
   };
 
-  const int code_end = min(u1, n_code), wide_begin = max(u0 - n_code, 0), wide_end = min(u1 - n_code, n_wide);
-  // against 16-bit rows the query is two bfloat16 terms, 16 bits; where registers allow, made together with the digits
-  constexpr bool kKeep16 = W == 16;
+  // against 16-bit rows the query is two bfloat16 terms, 16 bits
+  // up to 16 rows: the wavefronts' sums over cached rows are merged before they are rotated back, once
+  constexpr bool kMergeFirst = W == 16;
   u32x4 q_hi[NC], q_lo[NC];
-  const int wide_first = wide_begin + (MANY ? 0 : WK - 1 - wk);  // (the last wavefronts have the fewest code rows)
   auto split_query = [&](const float (&x)[8 * NC]) {
 #pragma unroll
     for (int k = 0; k < NC; ++k)
@@ -418,7 +474,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
   };
 
   // ================= code rows =================
-  if (MANY ? u0 < code_end : u0 + wk < code_end) {
+  if (group_begin < n_code) {  // uniform over the workgroup
     // Query digits.  A lane's inner slots of a product are what ExpandF4 makes of two code words: slot v is word v / 16, field f = 2 (v % 8) +
     // (v / 8) % 2, channel 32 (2w + f / 8) + 8c + f % 8 of the words' chunk c, where W = 32: product 0 takes words w = 0 of chunks
     // c = h and 2 + h, product 1 their words w = 1 (a group each where there are two); W = 16: one product, words 0 and 1 of chunk q.
@@ -454,7 +510,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
         return *reinterpret_cast<const u32x4 *>(blk + 4 * lane);
       }
     };
-    const int first = u0 + wk;
+    const int first = code_begin;
     // few rows, bound by the stream: two sets of registers, each asked for as a whole, the first in front of the query's preparation.  Page numbers
     // by scalar loads (the constant address space), whose wait stands in front of the first use: a vector load of a single one would be
     // waited for where it is issued, and every other load with it.
@@ -462,16 +518,21 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
     auto page_of = [&](int blk) { return page_at[min(blk * 32, s.len - 1) >> c.page_shift]; };
     MetaWords<NG> few_words[2];
     u32x4 few_k[2], few_v[2];
-    auto ask_few = [&](const Where &at, int x) {
-      load_meta(at, few_words[x]);
+    auto ask_codes = [&](const Where &at, int x) {
       few_k[x] = load_codes(c.k_codes, at);
       few_v[x] = load_codes(c.v_codes, at);
     };
-    int few_page = 0;
+    const int few_last = max(code_end, first + 1) - 1;  // (a wavefront without code rows asks for some block that there is)
+    Where behind = {};                                  // of the next block
+    int few_page = 0;                                   // of the one after that
     if constexpr (!MANY) {
-      const int page = page_of(first);
-      few_page = page_of(min(first + WK, n_code - 1));
-      ask_few(find(first, page), 0);
+      const int page = page_of(min(first, n_code - 1)), next_page = page_of(min(first + 1, min(few_last, n_code - 1)));
+      few_page = page_of(min(first + 2, min(few_last, n_code - 1)));
+      const Where at = find(min(first, n_code - 1), page);
+      load_meta(at, few_words[0]);
+      ask_codes(at, 0);
+      behind = find(min(first + 1, min(few_last, n_code - 1)), next_page);
+      load_meta(behind, few_words[1]);
     }
     u32x6 digits[NP][kDigits];
     uint32_t unit_exp;
@@ -483,7 +544,6 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
     {
       float x[8 * NC], mx = 0.0f;
       rotated(x);
-      if constexpr (kKeep16) split_query(x);
 #pragma unroll
       for (int e = 0; e < 8 * NC; ++e) mx = fmaxf(mx, fabsf(x[e]));
       mx = T::column_max(mx);
@@ -501,23 +561,44 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
         sum[e / (4 * NC)] += t - kMagic;  // (the upper half of a lane's channels is the second group)
         v[e] = (__float_as_int(t) + (kHalf - 0x4B400000)) ^ kHalf;
       }
+      auto make_digit = [&](int pr, int shift, int bits) {
+        f32x16 dig[2];  // even and odd slots, as the packing conversion takes them
 #pragma unroll
-      for (int pr = 0; pr < NP; ++pr)
-#pragma unroll
-        for (int d = 0; d < kDigits; ++d) {
-          f32x16 dig[2];  // even and odd slots, as the packing conversion takes them
-#pragma unroll
-          for (int slot = 0; slot < 32; ++slot) {
-            const int f = 2 * (slot & 7) + ((slot >> 3) & 1), word = slot >> 4;
-            // W = 32: x[16 m + 8 s + i] with m = 2 pr + f / 8, s = word; W = 16: x[8 m + i] with m = 2 word + f / 8
-            const int e = kWide ? 16 * (2 * pr + (f >> 3)) + 8 * word + (f & 7) : 8 * (2 * word + (f >> 3)) + (f & 7);
-            dig[slot & 1][slot >> 1] = (float)(d == kDigits - 1 ? v[e] >> (5 * d) : (int)__builtin_amdgcn_sbfe(v[e], 5 * d, 5));
-          }
-          digits[pr][d] = __builtin_bit_cast(u32x6, __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(dig[0], dig[1], 8.0f));
-          // The conversion reads its operands while it already writes: they are kept past it, so that the result gets registers of its own.
-          // (And one digit after the other: all of them at once take 128 registers.)
-          asm volatile("" ::"v"(dig[0]), "v"(dig[1]), "v"(digits[pr][d]) : "memory");
+        for (int slot = 0; slot < 32; ++slot) {
+          const int f = 2 * (slot & 7) + ((slot >> 3) & 1), word = slot >> 4;
+          // W = 32: x[16 m + 8 s + i] with m = 2 pr + f / 8, s = word; W = 16: x[8 m + i] with m = 2 word + f / 8
+          const int e = kWide ? 16 * (2 * pr + (f >> 3)) + 8 * word + (f & 7) : 8 * (2 * word + (f >> 3)) + (f & 7);
+          dig[slot & 1][slot >> 1] = (float)(int)__builtin_amdgcn_sbfe(v[e], shift, bits);
         }
+        const u32x6 made = __builtin_bit_cast(u32x6, __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(dig[0], dig[1], 8.0f));
+        // The conversion reads its operands while it already writes: they are kept past it, so that the result gets registers of its own.
+        // (And one digit after the other: all of them at once take 128 registers.)
+        asm volatile("" ::"v"(dig[0]), "v"(dig[1]), "v"(made) : "memory");
+        return made;
+      };
+      constexpr int kTop = 5 * (kDigits - 1);
+      if constexpr (MANY) {
+#pragma unroll
+        for (int pr = 0; pr < NP; ++pr)
+#pragma unroll
+          for (int d = 0; d < kDigits; ++d) digits[pr][d] = make_digit(pr, 5 * d, d == kDigits - 1 ? 32 - kTop : 5);
+      } else {  // the wavefronts have the same rows: a digit each
+        static_assert(kDigits <= kFewWaves);
+#pragma unroll
+        for (int pr = 0; pr < NP; ++pr) {
+          const u32x6 made = make_digit(pr, 5 * wave, wave == kDigits - 1 ? 32 - kTop : 5);
+#pragma unroll
+          for (int i = 0; i < 6; ++i) sh.digits[pr][wave][i][lane] = made[i];
+        }
+        lds_barrier();
+#pragma unroll
+        for (int pr = 0; pr < NP; ++pr)
+#pragma unroll
+          for (int d = 0; d < kDigits; ++d)
+#pragma unroll
+            for (int i = 0; i < 6; ++i) digits[pr][d][i] = sh.digits[pr][d][i][lane];
+        lds_barrier();  // (what comes last lies where the digits were)
+      }
       sum[0] *= u;
       sum[1] *= u;
       const float s0 = T::column_sum(NG == 2 ? sum[0] : sum[0] + sum[1]);
@@ -744,18 +825,22 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
       }
       lds_barrier();  // the stages of 16-bit rows lie where the blocks were
     } else {
-      BlockMeta<NG> &bm = sh.meta[0][wave];
-      for (int blk = first; blk < code_end; blk += 2 * WK) {
+      // A block's codes are asked for while the one before is worked on, its meta words a block earlier: they are decoded while the one before
+      // is worked on.
+      auto &bms = sh.own[wave].meta;
+      if (first < code_end) decode_block<NG>(few_words[0], first, bms[0], lane);
+      wave_lds_sync();
+      for (int blk = first; blk < code_end; blk += 2) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const int now = blk + x * WK;
+          const int now = blk + x;
           if (now >= code_end) break;
-          const Where at = find(min(now + WK, n_code - 1), few_page);
-          few_page = page_of(min(now + 2 * WK, n_code - 1));
-          ask_few(at, 1 - x);
-          wave_lds_sync();  // the block before is done with its words
-          decode_block<NG>(few_words[x], now, bm, lane);
-          wave_lds_sync();
+          ask_codes(behind, 1 - x);
+          behind = find(min(now + 2, few_last), few_page);
+          few_page = page_of(min(now + 3, few_last));
+          load_meta(behind, few_words[x]);
+          decode_block<NG>(few_words[1 - x], min(now + 1, few_last), bms[1 - x], lane);
+          const BlockMeta<NG> &bm = bms[x];
           float y[NY];
           scores(bm, y, [&](int pr, int half) {
             if constexpr (kWide) {
@@ -770,6 +855,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
           raise_codes(y);
           weights(bm, y);
           values(few_v[x], bm, y);
+          wave_lds_sync();
         }
       }
     }
@@ -832,7 +918,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
 
   // ================= 16-bit rows of the cache =================
   if (wide_begin < wide_end) {
-    if (!kKeep16 || u0 + wk >= code_end) {
+    {
       float x[8 * NC];
       rotated(x);
       split_query(x);
@@ -885,14 +971,14 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
                               [&](int nb, int g) { return *reinterpret_cast<const u32x4 *>(&sh.v[buf][x * 4096 + nb * 512 + 8 * (16 * g + n)]); });
              });
     } else {
-      for (int blk = wide_first; blk < wide_end; blk += WK)
+      for (int blk = wide_begin; blk < wide_end; ++blk)
         wide_block(blk, [&](int half, int k) { return *reinterpret_cast<const u32x4 *>(ks + (size_t)(blk * 32 + 16 * half + col) * kD + kD / NC * k + 8 * g_lane); },
                    [&](int nb, int g) { return *reinterpret_cast<const u32x4 *>(vs + (size_t)blk * 4096 + nb * 512 + 8 * (16 * g + n)); });
     }
   }
   // The cached rows' share is rotated back (H is its own inverse), and the chunk's rows join it.  Their weights are relative to the
   // sum so far: the reference of the code rows holds V scales as well.
-  if (!idle && (u0 + wk < code_end || wide_first < wide_end)) {
+  if (!kMergeFirst && !idle && (code_begin < code_end || wide_begin < wide_end)) {
     constexpr int NO = kWide ? 16 : 4;
     if (!a.out_rotated) {
       float x[NB * NO];
@@ -913,8 +999,23 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
     }
   }
 
+  if constexpr (kMergeFirst) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      *reinterpret_cast<f32x4 *>(&sh.own[wk].o[col][T::channel(j, 0, g_lane)]) = (f32x4){o[j][0], o[j][1], o[j][2], o[j][3]};
+      o[j] = T::zero();
+    }
+    const float sum = T::column_sum(l);
+    if (g_lane == 0) {
+      sh.m[wk][col] = limit < 0.0f ? kNoScore : m;
+      sh.l[wk][col] = sum;
+    }
+    m = 0.0f;
+    limit = 0.5f * kNoScore;
+    l = 0.0f;
+  }
+
   // ================= rows of the chunk =================
-  const int self_begin = max(u0 - n_code - n_wide, 0), self_end = min(u1 - n_code - n_wide, n_self);
   if (self_begin < self_end) {
     const int low_token = row0 / R;                                        // of this wavefront's rows
     const int my_end = idle ? 0 : (min(row0 + W, rows) - 1) / R / 32 + 1;
@@ -979,8 +1080,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
                }
              });
     } else {
-      uint16_t *vt = sh.v[wave];
-      for (int blk = self_begin + WK - 1 - wk; blk < min(self_end, my_end); blk += WK) {
+      uint16_t *vt = sh.v[W == 16 ? 0 : wave];
+      for (int blk = self_begin; blk < min(self_end, my_end); ++blk) {
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           const int row = 4 * x + (lane >> 4);
@@ -1019,6 +1120,60 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
       for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int x = 0; x < (kWide ? 4 : 1); ++x) store(row0 + col, T::channel(j, x, g_lane), part_of(j, x), m, l);
+  } else if constexpr (kMergeFirst) {
+    const bool with_self = group_begin <= self_at && run_start(split * WK + WK) > self_at;  // uniform: this workgroup has the chunk's block
+    if (self_begin < self_end) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x4 *>(&sh.self[col][T::channel(j, 0, g_lane)]) = part_of(j, 0);
+      if (g_lane == 0) { sh.m[WK][col] = m; sh.l[WK][col] = l; }
+    }
+    __syncthreads();
+    // Sixteen lanes a row, eight channels each.  Lanes meet at distances of 1, 2, 7 and 15 (what the lane exchanges of a row reach), so
+    // lane i takes chunk `place`, whose bits say how often each of them goes into i.
+    const int r = threadIdx.x >> 4, i = threadIdx.x & 15;
+    const int i1 = i ^ ((i & 8) ? 15 : 0), i2 = i1 ^ ((i1 & 4) ? 7 : 0), place = (i & 8) | (i1 & 4) | (i2 & 3), ch = 8 * place;
+    float top = sh.m[0][r], sum = 0.0f, x[8];
+#pragma unroll
+    for (int w = 1; w < WK; ++w) top = fmaxf(top, sh.m[w][r]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WK; ++w) {
+      const float f = exp2_bare(sh.m[w][r] - top);
+      sum += f * sh.l[w][r];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += f * sh.own[w].o[r][ch + e];
+    }
+    if (!a.out_rotated) {
+      butterflies(x, 1);
+      butterflies(x, 2);
+      butterflies(x, 4);
+      auto across = [&](auto exchange, int bit) {
+        const float sign = (place & bit) ? -1.0f : 1.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int other = __builtin_amdgcn_update_dpp(0, __float_as_int(x[e]), decltype(exchange)::value, 0xF, 0xF, false);
+          x[e] = __builtin_fmaf(sign, x[e], __int_as_float(other));
+        }
+      };
+      across(Dpp<0xB1>(), 1);   // quad_perm [1,0,3,2]
+      across(Dpp<0x4E>(), 2);   // quad_perm [2,3,0,1]
+      across(Dpp<0x141>(), 4);  // row_half_mirror
+      across(Dpp<0x140>(), 8);  // row_mirror
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= inv_sqrt128();
+    }
+    if (with_self) {
+      const float self_m = sh.m[WK][r], all = fmaxf(top, self_m), f = exp2_bare(top - all), g = exp2_bare(self_m - all);
+      sum = f * sum + g * sh.l[WK][r];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = f * x[e] + g * sh.self[r][ch + e];
+      top = all;
+    }
+    if (row0 + r < rows) {
+      store(row0 + r, ch, (f32x4){x[0], x[1], x[2], x[3]}, top, sum);
+      store(row0 + r, ch + 4, (f32x4){x[4], x[5], x[6], x[7]}, top, sum);
+    }
   } else {
     __syncthreads();  // (the sums lie where other wavefronts may still read)
 #pragma unroll
@@ -1045,26 +1200,52 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), 2) void paged
   }
 }
 
-// Merges the splits of a row: one wavefront a row, two channels a lane.
+// Merges the splits of a row: one wavefront a row, four channels a lane, the halves of the lanes take every other split.  Sixteen splits are in
+// flight at a time: one round trip to memory is all that most calls wait for.
 __global__ __launch_bounds__(256) void paged_combine_kernel(PagedAttentionArgs a) {
   const PagedArgs &c = a.c;
-  const int lane = threadIdx.x & 63, unit = blockIdx.y, b = unit / c.Hkv, head = unit % c.Hkv, R = a.Hq / c.Hkv;
+  const int lane = threadIdx.x & 63, half = lane >> 5, unit = blockIdx.y, b = unit / c.Hkv, head = unit % c.Hkv, R = a.Hq / c.Hkv;
   const int row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const ChunkSpan s = chunk_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
   if (row >= s.rows * R) return;
-  const int token = row / R, hq = head * R + row - token * R;
+  const int token = row / R, hq = head * R + row - token * R, ch = 4 * (lane & 31);
   const size_t at = (size_t)(s.first + token) * a.Hq + hq;
   const float *p = a.partial + at * a.n_split * kPartialStride;
-  float top = kNoScore, sum = 0.0f, x0 = 0.0f, x1 = 0.0f;
-  for (int i = 0; i < a.n_split; ++i) top = fmaxf(top, p[i * kPartialStride]);
-  for (int i = 0; i < a.n_split; ++i) {
-    const float *r = p + i * kPartialStride, f = exp2_bare(r[0] - top);
-    sum += f * r[1];
-    x0 += f * r[4 + 2 * lane];
-    x1 += f * r[5 + 2 * lane];
+  float top = kNoScore, sum = 0.0f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int from = 0; from < a.n_split; from += 16) {
+    float m[8], l[8];
+    f32x4 part[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool there = from + 2 * i + half < a.n_split;
+      const float *r = p + (there ? from + 2 * i + half : from) * kPartialStride;
+      m[i] = there ? r[0] : kNoScore;
+      l[i] = there ? r[1] : 0.0f;
+      part[i] = *reinterpret_cast<const f32x4 *>(r + 4 + ch);
+    }
+    float all = top;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) all = fmaxf(all, m[i]);
+    all = halves_max(all);
+    const float alpha = exp2_bare(top - all);
+    top = all;
+    sum *= alpha;
+    x *= alpha;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float f = from + 2 * i + half < a.n_split ? exp2_bare(m[i] - all) : 0.0f;
+      sum = __builtin_fmaf(f, l[i], sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(f, part[i][e], x[e]);
+    }
   }
+  sum = halves_sum(sum);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = halves_sum(x[e]);
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-  *reinterpret_cast<uint32_t *>(a.out + (s.first + token) * a.out_stride + hq * kD + 2 * lane) = pack_f16x2(x0 * inv, x1 * inv);
+  if (half == 0)
+    *reinterpret_cast<u32x2 *>(a.out + (s.first + token) * a.out_stride + hq * kD + ch) = (u32x2){pack_f16x2(x[0] * inv, x[1] * inv), pack_f16x2(x[2] * inv, x[3] * inv)};
   if (a.lse && lane == 0) a.lse[at] = sum > 0.0f ? (top + log2_bare(sum)) * kLn2 : -INFINITY;
 }
 
