@@ -230,63 +230,69 @@ struct BlockMeta {
   __attribute__((aligned(16))) float v_rcp[32];                       // 4^ii / V scale, the larger one where there are two (no part: 0)
   __attribute__((aligned(16))) float v_share[NG == 2 ? 2 : 1][32];    // V scale / the larger one
   __attribute__((aligned(16))) uint16_t v_zero[2][NG][32];            // binary16, in the weights' order: zero-point * 4^(ii - 3), low part and multiples of 2048
-  int far;                                                            // some zero-point has such multiples
 };
 
 template <int NG>
-struct MetaWords {
-  uint32_t w[NG];  // lanes 0-31: K meta of row `lane`, lanes 32-63: V meta of row lane - 32
-  int limit;       // rows from here on (of the sequence) take no part
-};
+struct MetaWords { uint32_t w[NG]; };
 
-// The common part: what scores and the denominator need.  PLACES: the factors 4^ii of values that stay in their words' places.
-template <int NG, bool PLACES, typename Meta>
-__device__ __forceinline__ void decode_meta(const MetaWords<NG> &cur, int blk, Meta &bm, int lane, float (&scale)[NG], float (&zero)[NG], float &rcp) {
-  const int r = lane & 31, ii = r & 3;
-  const bool part = blk * 32 + r < cur.limit && (cur.w[0] & 0x8000u) == 0u;
-#pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    scale[g] = part ? half_bits_to_float(cur.w[g] & 0x7FFFu) : 1.0f;
-    zero[g] = part ? (float)((int)cur.w[g] >> 16) : 0.0f;
-  }
-  const float top = NG == 2 && lane >= 32 ? fmaxf(scale[0], scale[NG - 1]) : scale[0];
-  rcp = part ? __builtin_amdgcn_rcpf(top) : 0.0f;
-  const float v_log = halves(log2_bare(top)).hi - (PLACES ? 2.0f * (float)ii : 0.0f);  // (keys' lanes: of their row's values)
-  if (lane < 32) {
-    const Terms inv = split_terms(rcp), log = split_terms(part ? v_log * rcp : kNoScore);
-    const float zh = rintf(zero[0] * (1.0f / 256.0f)) * -256.0f, zl = -zero[0] - zh;
-    u32x4 *to = reinterpret_cast<u32x4 *>(&bm.start[r][0][0]);
-    to[0] = (u32x4){upper_halves(zl, zl), upper_halves(zl, zh), upper_halves(zh, zh), upper_halves(log.a, log.b)};
-    to[1] = (u32x4){upper_halves(inv.a, inv.a), upper_halves(inv.a, inv.b), upper_halves(inv.b, inv.c), upper_halves(log.c, 0.0f)};
-    if constexpr (NG == 2) {
-      const float yh = rintf(zero[1] * (1.0f / 256.0f)) * -256.0f, yl = -zero[1] - yh;
-      *reinterpret_cast<u32x4 *>(&bm.start2[r][0]) = (u32x4){upper_halves(yl, yl), upper_halves(yl, yh), upper_halves(yh, yh), 0u};
-    }
-#pragma unroll
-    for (int g = 0; g < NG; ++g) bm.k_scale[g][r] = part || g == 0 ? scale[g] : 0.0f;
+template <int NG>
+__device__ __forceinline__ MetaWords<NG> load_meta(const uint32_t *at) {
+  if constexpr (NG == 2) {
+    const u32x2 w = *reinterpret_cast<const u32x2 *>(at);
+    return {{w[0], w[1]}};
   } else {
-    bm.v_rcp[r] = rcp * (PLACES ? (float)(1 << (2 * ii)) : 1.0f);
+    return {{*at}};
   }
 }
-// ... and what values need that stay in their words
+// A row's scales and zero-points; one that takes no part has a scale of 1 and nothing else
 template <int NG>
-__device__ __forceinline__ void decode_block(const MetaWords<NG> &cur, int blk, BlockMeta<NG> &bm, int lane) {
-  float scale[NG], zero[NG], rcp;
-  decode_meta<NG, true>(cur, blk, bm, lane, scale, zero, rcp);
-  const int r = lane & 31, ii = r & 3;
-  bool far = false;  // a zero-point that 11 bits do not hold
-  if (lane >= 32) {
-    const int at = 2 * (4 * ((r & 15) >> 2) + ii) + (r >> 4);  // the weights' order: pairs (r, r + 16)
+struct RowMeta {
+  float scale[NG], zero[NG], top, rcp;  // the larger scale and its reciprocal (no part: 0)
+  bool part;
+  __device__ __forceinline__ RowMeta(const MetaWords<NG> &m, bool there, bool value) {
+    part = there && (m.w[0] & 0x8000u) == 0u;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      if constexpr (NG == 2) bm.v_share[g][r] = scale[g] * rcp;
-      const float hi = rintf(zero[g] * (1.0f / 2048.0f)) * 2048.0f, f = (float)(1 << (2 * ii)) * (1.0f / 64.0f);
-      bm.v_zero[0][g][at] = (uint16_t)float_to_half_bits_rne((zero[g] - hi) * f);
-      bm.v_zero[1][g][at] = (uint16_t)float_to_half_bits_rne(hi * f);
-      far = far || hi != 0.0f;
+      scale[g] = part ? half_bits_to_float(m.w[g] & 0x7FFFu) : 1.0f;
+      zero[g] = part ? (float)((int)m.w[g] >> 16) : 0.0f;
     }
+    top = NG == 2 && value ? fmaxf(scale[0], scale[NG - 1]) : scale[0];  // (keys: the first group's)
+    rcp = part ? __builtin_amdgcn_rcpf(top) : 0.0f;
   }
-  bm.far = __ballot(far) != 0ull;
+};
+// What scores need of a key's row; v_log: base-2 logarithm of what its value is multiplied by
+template <int NG, typename Meta>
+__device__ __forceinline__ void decode_key(const RowMeta<NG> &k, float v_log, Meta &bm, int r) {
+  const Terms inv = split_terms(k.rcp), log = split_terms(k.part ? v_log * k.rcp : kNoScore);
+  const float zh = rintf(k.zero[0] * (1.0f / 256.0f)) * -256.0f, zl = -k.zero[0] - zh;
+  u32x4 *to = reinterpret_cast<u32x4 *>(&bm.start[r][0][0]);
+  to[0] = (u32x4){upper_halves(zl, zl), upper_halves(zl, zh), upper_halves(zh, zh), upper_halves(log.a, log.b)};
+  to[1] = (u32x4){upper_halves(inv.a, inv.a), upper_halves(inv.a, inv.b), upper_halves(inv.b, inv.c), upper_halves(log.c, 0.0f)};
+  if constexpr (NG == 2) {
+    const float yh = rintf(k.zero[1] * (1.0f / 256.0f)) * -256.0f, yl = -k.zero[1] - yh;
+    *reinterpret_cast<u32x4 *>(&bm.start2[r][0]) = (u32x4){upper_halves(yl, yl), upper_halves(yl, yh), upper_halves(yh, yh), 0u};
+  }
+#pragma unroll
+  for (int g = 0; g < NG; ++g) bm.k_scale[g][r] = k.part || g == 0 ? k.scale[g] : 0.0f;
+}
+// Two blocks' meta words for values that stay in their words, a row a lane.  Returns whether some zero-point takes more than 11 bits.
+template <int NG>
+__device__ __forceinline__ bool decode_pair(const MetaWords<NG> &kw, const MetaWords<NG> &vw, bool there, BlockMeta<NG> (&pair)[2], int lane) {
+  const int r = lane & 31, ii = r & 3, at = 2 * (4 * ((r & 15) >> 2) + ii) + (r >> 4);  // the weights' order: pairs (r, r + 16)
+  BlockMeta<NG> &bm = pair[lane >> 5];
+  const RowMeta<NG> v(vw, there, true), k(kw, there, false);
+  decode_key(k, log2_bare(v.top) - 2.0f * (float)ii, bm, r);
+  bm.v_rcp[r] = v.rcp * (float)(1 << (2 * ii));
+  bool far = false;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    if constexpr (NG == 2) bm.v_share[g][r] = v.scale[g] * v.rcp;
+    const float hi = rintf(v.zero[g] * (1.0f / 2048.0f)) * 2048.0f, f = (float)(1 << (2 * ii)) * (1.0f / 64.0f);
+    bm.v_zero[0][g][at] = (uint16_t)float_to_half_bits_rne((v.zero[g] - hi) * f);
+    bm.v_zero[1][g][at] = (uint16_t)float_to_half_bits_rne(hi * f);
+    far = far || hi != 0.0f;
+  }
+  return __ballot(far) != 0ull;
 }
 
 // A block expanded for the wavefronts of a workgroup of many rows: operands as their lanes take them.
@@ -322,24 +328,26 @@ struct PagedShared<G, W, true> {
 };
 template <int G>
 struct PagedShared<G, 16, false> {
-  union {  // of every wavefront its own: a block's meta words and the next one's, then its sums
-    BlockMeta<kD / G> meta[2];
+  union {  // of every wavefront its own: a pair of blocks' meta words and the next one's, then its sums
+    BlockMeta<kD / G> meta[2][2];
     __attribute__((aligned(16))) float o[16][kD + 4];
   } own[kFewWaves];
-  union {
+  union {  // one after the other; (sixteen rows of a unit are of one block of the chunk)
     uint32_t digits[1][kDigits][6][kWave];
+    __attribute__((aligned(16))) uint16_t v[1][32 * kD];
     __attribute__((aligned(16))) float self[16][kD + 4];  // sums over the chunk's rows
   };
-  __attribute__((aligned(16))) uint16_t v[1][32 * kD];    // (sixteen rows of a unit are of one block of the chunk)
   float m[kFewWaves + 1][16], l[kFewWaves + 1][16];
 };
 template <int G>
 struct PagedShared<G, 32, false> {
   union {  // the sums of the wavefronts come last
     struct {
-      struct { BlockMeta<kD / G> meta[2]; } own[kFewWaves];
-      __attribute__((aligned(16))) uint16_t v[kFewWaves][32 * kD];
-      uint32_t digits[2][kDigits][6][kWave];
+      struct { BlockMeta<kD / G> meta[2][2]; } own[kFewWaves];
+      union {
+        __attribute__((aligned(16))) uint16_t v[kFewWaves][32 * kD];
+        uint32_t digits[2][kDigits][6][kWave];
+      };
     };
     __attribute__((aligned(16))) float o[kFewWaves][32][kD + 4];
   };
@@ -429,10 +437,13 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
   };
   // A block's scores relative to the reference (no part: far below).  The reference is raised, and what was summed against it rescaled
   // (`more`: the rest of it), only when a score exceeds it by kRaiseAt.
-  auto raise = [&](float (&y)[NY], auto &&more) {
-    float top = y[0];
+  auto raise = [&](auto &&more, auto &...y) {
+    float top = kNoScore;
+    auto top_of = [&](float (&x)[NY]) {
 #pragma unroll
-    for (int i = 1; i < NY; ++i) top = fmaxf(top, y[i]);
+      for (int i = 0; i < NY; ++i) top = fmaxf(top, x[i]);
+    };
+    (top_of(y), ...);
     if (__builtin_expect(__ballot(top > limit) != 0ull, 0)) {
       const float all = T::column_max(top);
       float by = 0.0f;
@@ -447,12 +458,15 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
         limit = kRaiseAt;
         more(alpha);
       }
+      auto lower = [&](float (&x)[NY]) {
 #pragma unroll
-      for (int i = 0; i < NY; ++i) y[i] -= by;
+        for (int i = 0; i < NY; ++i) x[i] -= by;
+      };
+      (lower(y), ...);
     }
   };
   auto weigh = [&](float (&y)[NY]) {  // ... and their weights
-    raise(y, [](float) {});
+    raise([](float) {}, y);
 #pragma unroll
     for (int i = 0; i < NY; ++i) y[i] = exp2_bare(y[i]);
   };
@@ -490,16 +504,6 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       const bool there = page >= 0 && page < c.n_pages;
       return Where{(((size_t)(there ? page : 0) * c.Hkv + head) << c.page_shift) + ((blk * 32) & ((1 << c.page_shift) - 1)), there ? s.len : 0};
     };
-    auto load_meta = [&](const Where &at, MetaWords<NG> &t) {
-      const uint32_t *meta = (lane < 32 ? c.k_meta : c.v_meta) + (at.row + (lane & 31)) * NG;
-      if constexpr (NG == 2) {
-        const u32x2 w = *reinterpret_cast<const u32x2 *>(meta);
-        t.w[0] = w[0]; t.w[1] = w[1];
-      } else {
-        t.w[0] = *meta;
-      }
-      t.limit = at.limit;
-    };
     // W = 32: words 2p and 2p + 1 of chunks h and 2 + h (the other half of the lanes takes the other two); W = 16: all words of a chunk
     auto load_codes = [&](const uint32_t *pool, const Where &at) {
       const uint32_t *blk = pool + at.row * 8;
@@ -511,28 +515,50 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       }
     };
     const int first = code_begin;
-    // few rows, bound by the stream: two sets of registers, each asked for as a whole, the first in front of the query's preparation.  Page numbers
-    // by scalar loads (the constant address space), whose wait stands in front of the first use: a vector load of a single one would be
-    // waited for where it is issued, and every other load with it.
-    const auto *page_at = reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(table));
-    auto page_of = [&](int blk) { return page_at[min(blk * 32, s.len - 1) >> c.page_shift]; };
-    MetaWords<NG> few_words[2];
-    u32x4 few_k[2], few_v[2];
-    auto ask_codes = [&](const Where &at, int x) {
-      few_k[x] = load_codes(c.k_codes, at);
-      few_v[x] = load_codes(c.v_codes, at);
+    // Few rows, bound by the stream: blocks in pairs, whose rows' meta words are decoded a row a lane.  Keys and values of the next pair are asked
+    // for as soon as this one's are used up, meta words of the one after it in front of them, and the first ones in front of the query's
+    // preparation.  The pages' numbers come 64 at a time (lane l: of block window + l), another 64 ahead: one a block, by a scalar load,
+    // would be waited for with the next access to LDS.
+    const int few_last = min(max(code_end, first + 1), n_code) - 1;  // (a wavefront without code rows asks for some block that there is)
+    auto ask_pages = [&](int from, int last) { return table[min(min(from + lane, last) * 32, s.len - 1) >> c.page_shift]; };
+    int window = first, pages = 0, next_pages = 0;
+    struct Pair { Where at[2]; };
+    auto locate = [&](int blk) {  // in ascending order
+      Pair p;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int at = min(blk + x, few_last);
+        if (at - window >= kWave) {
+          window += kWave;
+          pages = next_pages;
+          next_pages = ask_pages(window + kWave, few_last);
+        }
+        p.at[x] = find(at, __builtin_amdgcn_readlane(pages, at - window));
+        if (blk + x >= code_end) p.at[x].limit = 0;
+      }
+      return p;
     };
-    const int few_last = max(code_end, first + 1) - 1;  // (a wavefront without code rows asks for some block that there is)
-    Where behind = {};                                  // of the next block
-    int few_page = 0;                                   // of the one after that
+    MetaWords<NG> few_kw, few_vw;
+    u32x4 few_k[2], few_v[2];
+    auto ask_meta = [&](const Pair &p) {
+      const size_t row = ((lane < 32 ? p.at[0].row : p.at[1].row) + (lane & 31)) * NG;
+      few_kw = load_meta<NG>(c.k_meta + row);
+      few_vw = load_meta<NG>(c.v_meta + row);
+    };
+    auto row_there = [&](int blk, const Pair &p) { return (blk + (lane >> 5)) * 32 + (lane & 31) < (lane < 32 ? p.at[0].limit : p.at[1].limit); };
+    Pair now = {}, next = {};
     if constexpr (!MANY) {
-      const int page = page_of(min(first, n_code - 1)), next_page = page_of(min(first + 1, min(few_last, n_code - 1)));
-      few_page = page_of(min(first + 2, min(few_last, n_code - 1)));
-      const Where at = find(min(first, n_code - 1), page);
-      load_meta(at, few_words[0]);
-      ask_codes(at, 0);
-      behind = find(min(first + 1, min(few_last, n_code - 1)), next_page);
-      load_meta(behind, few_words[1]);
+      window = min(first, few_last);
+      pages = ask_pages(window, few_last);
+      next_pages = ask_pages(window + kWave, few_last);
+      now = locate(first);
+      ask_meta(now);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        few_k[x] = load_codes(c.k_codes, now.at[x]);
+        few_v[x] = load_codes(c.v_codes, now.at[x]);
+      }
+      next = locate(first + 2);
     }
     u32x6 digits[NP][kDigits];
     uint32_t unit_exp;
@@ -614,10 +640,9 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
 #pragma unroll
       for (int half = 0; half < (kWide ? 1 : 2); ++half) {
         const int row = kWide ? lane & 31 : 16 * half + n;  // of the row operands
-        const u32x4 none = {0u, 0u, 0u, 0u};
-        u32x4 first[NG];
-        first[0] = g_lane < 2 ? *reinterpret_cast<const u32x4 *>(&bm.start[row][g_lane & 1][0]) : none;
-        if constexpr (NG == 2) first[1] = g_lane == 0 ? *reinterpret_cast<const u32x4 *>(&bm.start2[row][0]) : none;
+        u32x4 first[NG];  // (lane groups without a slot to fill meet zeros in the column operand)
+        first[0] = *reinterpret_cast<const u32x4 *>(&bm.start[row][g_lane & 1][0]);
+        if constexpr (NG == 2) first[1] = *reinterpret_cast<const u32x4 *>(&bm.start2[row][0]);
         Acc acc[NG];
 #pragma unroll
         for (int g = 0; g < NG; ++g) acc[g] = T::bf16(first[g], start[g], T::zero());
@@ -643,12 +668,12 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
         }
       }
     };
-    auto raise_codes = [&](float (&y)[NY]) {
-      raise(y, [&](float alpha) {
+    auto raise_codes = [&](auto &...y) {
+      raise([&](float alpha) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) acc_z[g] *= alpha;
         if (g_lane == 1) start[0] = start_slots(-m, 0x00003F80u);
-      });
+      }, y...);
     };
     // weights of a block's scores, and their sum
     auto weights = [&](const auto &bm, float (&y)[NY]) {
@@ -667,8 +692,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       l += l2;
     };
     // values that stay in their words
-    [[maybe_unused]] auto values = [&](const u32x4 &v, const BlockMeta<NG> &bm, float (&y)[NY]) {
-      const int far = bm.far;
+    [[maybe_unused]] auto values = [&](const u32x4 &v, const BlockMeta<NG> &bm, bool far, float (&y)[NY]) {
       u32x4 w[NG][NS];
 #pragma unroll
       for (int g = 0; g < NG; ++g)
@@ -687,7 +711,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       // ---- zero-points: sums with the rounded weights
 #pragma unroll
       for (int x = 0; x < 2; ++x)
-        if (x == 0 || __builtin_expect(__builtin_amdgcn_readfirstlane(far) != 0, 0))
+        if (x == 0 || __builtin_expect(far, 0))
 #pragma unroll
           for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -716,7 +740,6 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       // second its keys and the other half.  What they need is asked for while the blocks before are worked on, and the pages'
       // numbers (lane l: of block from + l) a round earlier.
       const int mine = wave >> 1, part = wave & 1, h = g_lane;
-      auto ask_pages = [&](int from) { return table[min(min(from + lane, n_code - 1) * 32, s.len - 1) >> c.page_shift]; };
       MetaWords<NG> words;
       u32x4 k, v_meta[2][NG];
       u32x2 v;
@@ -729,14 +752,17 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
 #pragma unroll
           for (int y = 0; y < NG; ++y) v_meta[x][y] = *reinterpret_cast<const u32x4 *>(meta + 16 * NG * x + 4 * y);
         v = *reinterpret_cast<const u32x2 *>(c.v_codes + at.row * 8 + (16 * (2 * part + h) + n) * 4 + 2 * p);
-        if (part == 0) load_meta(at, words);
+        if (part == 0) words = load_meta<NG>((lane < 32 ? c.k_meta : c.v_meta) + (at.row + (lane & 31)) * NG);
         else k = load_codes(c.k_codes, at);
         limit = at.limit;
       };
       auto expand = [&](int blk, CodeBlock<NG> &to) {
         if (part == 0) {
-          float scale[NG], zero[NG], rcp;
-          decode_meta<NG, false>(words, blk, to, lane, scale, zero, rcp);
+          const int r = lane & 31;  // lanes 0-31: keys, lanes 32-63: values
+          const RowMeta<NG> row(words, blk * 32 + r < limit, lane >= 32);
+          const float v_log = halves(log2_bare(row.top)).hi;
+          if (lane < 32) decode_key(row, v_log, to, r);
+          else to.v_rcp[r] = row.rcp;
         } else {
           const u32x2 k0 = ex4(k[0]), k1 = ex4(k[1]), k2 = ex4(k[2]), k3 = ex4(k[3]);
           to.k[0][lane] = (u32x4){k0[0], k0[1], k2[0], k2[1]};
@@ -805,13 +831,13 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
           for (int j = 0; j < NB; ++j) o[j] = T::f16(bm.v[st][j][lane], w, o[j]);
         }
       };
-      int pages = ask_pages(first);
+      int pages = ask_pages(first, n_code - 1);
       ask(first, pages);
-      pages = ask_pages(first + kStageBlocks);
+      pages = ask_pages(first + kStageBlocks, n_code - 1);
       for (int from = first, turn = 0; from < code_end; from += kStageBlocks, turn ^= 1) {
         expand(min(from + mine, n_code - 1), sh.blocks[turn][mine]);
         ask(from + kStageBlocks, pages);
-        pages = ask_pages(from + 2 * kStageBlocks);
+        pages = ask_pages(from + 2 * kStageBlocks, n_code - 1);
         lds_barrier();  // (the other set was last read in front of the barrier before)
         if (idle) continue;
         const int last = min(kStageBlocks, code_end - from);
@@ -825,38 +851,57 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       }
       lds_barrier();  // the stages of 16-bit rows lie where the blocks were
     } else {
-      // A block's codes are asked for while the one before is worked on, its meta words a block earlier: they are decoded while the one before
-      // is worked on.
       auto &bms = sh.own[wave].meta;
-      if (first < code_end) decode_block<NG>(few_words[0], first, bms[0], lane);
+      auto codes_of = [&](int x) {
+        return [&, x](int pr, int half) {
+          if constexpr (kWide) {
+            const u32x2 lo = ex4(few_k[x][pr]), hi = ex4(few_k[x][2 + pr]);
+            return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+          } else {  // a group's product takes zeros in the other's slots
+            const u32x2 lo = ex4(few_k[x][2 * half]), hi = ex4(few_k[x][2 * half + 1]), none = {0u, 0u};
+            const u32x2 a0 = NG == 2 && pr == 1 ? none : lo, a1 = NG == 2 && pr == 0 ? none : hi;
+            return (u32x4){a0[0], a0[1], a1[0], a1[1]};
+          }
+        };
+      };
+      bool far = false;
+      if (first < code_end) far = decode_pair<NG>(few_kw, few_vw, row_there(first, now), bms[0], lane);
+      ask_meta(next);
       wave_lds_sync();
-      for (int blk = first; blk < code_end; blk += 2) {
+      for (int blk = first, turn = 0; blk < code_end; blk += 2, turn ^= 1) {
+        const bool next_far = decode_pair<NG>(few_kw, few_vw, row_there(blk + 2, next), bms[turn ^ 1], lane);
+        const Pair after = locate(blk + 4);
+        ask_meta(after);
+        const BlockMeta<NG> (&bm)[2] = bms[turn];
+        if constexpr (kWide) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int now = blk + x;
-          if (now >= code_end) break;
-          ask_codes(behind, 1 - x);
-          behind = find(min(now + 2, few_last), few_page);
-          few_page = page_of(min(now + 3, few_last));
-          load_meta(behind, few_words[x]);
-          decode_block<NG>(few_words[1 - x], min(now + 1, few_last), bms[1 - x], lane);
-          const BlockMeta<NG> &bm = bms[x];
-          float y[NY];
-          scores(bm, y, [&](int pr, int half) {
-            if constexpr (kWide) {
-              const u32x2 lo = ex4(few_k[x][pr]), hi = ex4(few_k[x][2 + pr]);
-              return (u32x4){lo[0], lo[1], hi[0], hi[1]};
-            } else {  // a group's product takes zeros in the other's slots
-              const u32x2 lo = ex4(few_k[x][2 * half]), hi = ex4(few_k[x][2 * half + 1]), none = {0u, 0u};
-              const u32x2 a0 = NG == 2 && pr == 1 ? none : lo, a1 = NG == 2 && pr == 0 ? none : hi;
-              return (u32x4){a0[0], a0[1], a1[0], a1[1]};
-            }
-          });
-          raise_codes(y);
-          weights(bm, y);
-          values(few_v[x], bm, y);
-          wave_lds_sync();
+          for (int x = 0; x < 2; ++x) {
+            if (x == 1 && blk + 1 >= code_end) break;
+            float y[NY];
+            scores(bm[x], y, codes_of(x));
+            few_k[x] = load_codes(c.k_codes, next.at[x]);
+            raise_codes(y);
+            weights(bm[x], y);
+            values(few_v[x], bm[x], far, y);
+            few_v[x] = load_codes(c.v_codes, next.at[x]);
+          }
+        } else {  // both at once: what one waits for the other covers
+          float y0[NY], y1[NY];
+          scores(bm[0], y0, codes_of(0));
+          scores(bm[1], y1, codes_of(1));
+#pragma unroll
+          for (int x = 0; x < 2; ++x) few_k[x] = load_codes(c.k_codes, next.at[x]);
+          raise_codes(y0, y1);
+          weights(bm[0], y0);
+          weights(bm[1], y1);
+          values(few_v[0], bm[0], far, y0);
+          values(few_v[1], bm[1], far, y1);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) few_v[x] = load_codes(c.v_codes, next.at[x]);
         }
+        next = after;
+        far = next_far;
+        wave_lds_sync();
       }
     }
     // codes were 2^-24 of themselves, zero-points 2^-6; a group's zero-points reach all of its channels
