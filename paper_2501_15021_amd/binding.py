@@ -174,6 +174,7 @@ def native():
         except ImportError as e:
             raise AkvqError(f"_akvq_torch is missing ({e}): run `python -m paper_2501_15021_amd.build` first") from e
         _akvq_torch.plain_cache(*_PLAIN, akvq_cache, akvq_window)
+        _akvq_torch.plain_paged(_PLAIN_PAGED, akvq_paged, AkvqError)
         _native = _akvq_torch
     return _native
 
@@ -405,22 +406,6 @@ def _need(ok: bool, what: str) -> None:
         raise AkvqError(what)
 
 
-def _on_device(*tensors) -> None:
-    """The calls go to the current device's stream: a tensor of another device (or of the host) is refused."""
-    here = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for t in tensors:
-        _need(t is None or (t.is_cuda and t.get_device() == here), "tensors have to be on the current device")
-
-
-def _packed(t: torch.Tensor, what: str, rows: Optional[int] = None, heads: Optional[int] = None) -> int:
-    """[rows, heads, 128] fp16 whose heads lie next to each other; returns the elements from row to row."""
-    _need(t.dtype == torch.float16 and t.dim() == 3 and t.shape[2] == D, f"{what} has to be fp16 [rows, heads, 128]")
-    _need((rows is None or t.shape[0] == rows) and (heads is None or t.shape[1] == heads), f"{what}: rows or heads do not fit")
-    n, h, _ = t.shape
-    _need(t.stride(2) == 1 and (h == 1 or t.stride(1) == D), f"{what}: the heads of a row have to lie next to each other")
-    return t.stride(0) if n > 1 else h * D
-
-
 class RopeAxes:
     """Frequencies of rotary positions with several axes: channel pair (i, i + 64) turns by pos[axis[i]] * inv_freq[i]."""
 
@@ -447,50 +432,23 @@ class RopeAxes:
             axis = [a for a, n in enumerate(sections) for _ in range(n)]
         return cls([theta ** (-i / 64) for i in range(64)], axis)
 
-    def _positions(self, pos: torch.Tensor, rows: int) -> int:
-        """Checks pos ([n_axes, rows], or [rows] for one axis); returns the elements from axis to axis."""
-        _need(pos.dtype == torch.int32 and pos.dim() in (1, 2), "positions have to be int32 [axes, rows]")
-        _need(pos.shape[-1] == rows and (pos.shape[0] >= self.n_axes if pos.dim() == 2 else self.n_axes == 1),
-              "positions: one entry for every axis and row")
-        _need(rows <= 1 or pos.stride(-1) == 1, "positions: the rows of an axis have to lie next to each other")
-        return pos.stride(0) if pos.dim() == 2 and pos.shape[0] > 1 else rows
-
 
 def rope_axes(axes: RopeAxes, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None,
               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False):
     """akvq_rope_axes: rotary positions of a chunk's rows, q [n, Hq, 128] and k [n, Hkv, 128] (either may be None), into q_out and k_out
     (new tensors where None; q and k themselves turn in place).  inverse: turns back, which is also the gradient.  Returns (q_out, k_out)."""
-    _need(q is not None or k is not None, "neither q nor k")
-    rows = (q if q is not None else k).shape[0]
-    args, outs = [], []
-    for x, out, what in ((q, q_out, "q"), (k, k_out, "k")):
-        if x is None:
-            _need(out is None, f"{what}_out without {what}")
-            args += [None, 0, 0, None, 0]
-        else:
-            stride = _packed(x, what, rows)
-            if out is None:
-                out = torch.empty(x.shape, dtype=torch.float16, device=x.device)
-            args += [x.data_ptr(), stride, x.shape[1], out.data_ptr(), _packed(out, what + "_out", rows, x.shape[1])]
-        outs.append(out)
-    pos_stride = axes._positions(pos, rows)
-    _on_device(pos, q, k, *outs)
-    if rows:
-        _check(lib().akvq_rope_axes(C.byref(axes._struct), pos.data_ptr(), pos_stride, rows, *args[:3], *args[5:8], *args[3:5],
-                                    *args[8:], ROPE_INVERSE if inverse else 0, _stream()), "akvq_rope_axes")
-    return tuple(outs)
+    st, outs = (_native or native()).rope_axes(axes._struct, pos, q, k, q_out, k_out, inverse)
+    if st:
+        _check(st, "akvq_rope_axes")
+    return outs
 
 
 def rope_axes_table(axes: RopeAxes, pos: torch.Tensor):
     """akvq_rope_axes_table: (cos, sin) [rows, 64] fp16 for the calls that take rope=(cos, sin)."""
-    rows = pos.shape[-1]
-    pos_stride = axes._positions(pos, rows)
-    _on_device(pos)
-    cos, sin = (torch.empty(rows, 64, dtype=torch.float16, device=pos.device) for _ in range(2))
-    if rows:
-        _check(lib().akvq_rope_axes_table(C.byref(axes._struct), pos.data_ptr(), pos_stride, rows, cos.data_ptr(), sin.data_ptr(),
-                                          _stream()), "akvq_rope_axes_table")
-    return cos, sin
+    st, table = (_native or native()).rope_axes_table(axes._struct, pos)
+    if st:
+        _check(st, "akvq_rope_axes_table")
+    return table
 
 
 class PagedCache:
@@ -536,24 +494,16 @@ class PagedCache:
     workspace, counts, nbytes = Cache.workspace, Cache.counts, Cache.nbytes
 
 
-def _chunk(cache: PagedCache, row_start: torch.Tensor, rows: int, max_rows: int) -> akvq_chunk:
-    _need(row_start.dtype == torch.int32 and row_start.dim() == 1 and row_start.shape[0] == cache.B + 1 and row_start.is_contiguous(),
-          "row_start has to be int32 [sequences + 1]")
-    _need(max_rows >= 0, "max_rows has to be at least 0")
-    return akvq_chunk(row_start.data_ptr(), rows, max_rows)
+_PLAIN_PAGED = PagedCache.paged_struct  # as _PLAIN
 
 
 def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int, clip: float,
                  flags: int = 0) -> None:
     """akvq_paged_append: rows k, v [n, Hkv, 128] fp16 of a chunk, row_start[b] to row_start[b + 1] those of sequence b (max_rows at
     most), become its cache rows from seq_len[b] on.  cache.seq_len is the caller's to advance."""
-    rows = k.shape[0]
-    ks, vs = _packed(k, "k", heads=cache.Hkv), _packed(v, "v", rows, cache.Hkv)
-    c, chunk = cache.paged_struct(), _chunk(cache, row_start, rows, max_rows)
-    _on_device(cache.k_codes, k, v, row_start)
-    if rows:
-        _check(lib().akvq_paged_append(C.byref(c), C.byref(chunk), k.data_ptr(), ks, v.data_ptr(), vs, clip, flags, _stream()),
-               "akvq_paged_append")
+    st = (_native or native()).paged_append(cache, k, v, row_start, max_rows, clip, flags)
+    if st:
+        _check(st, "akvq_paged_append")
 
 
 def paged_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int,
@@ -561,23 +511,9 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torc
                     lse: Optional[torch.Tensor] = None) -> torch.Tensor:
     """akvq_paged_attention: a chunk's rows q [n, Hq, 128], k and v [n, Hkv, 128] fp16 (row_start and max_rows as in paged_append) over the
     cached rows of their sequences and over the chunk's own rows up to each.  Returns out [n, Hq, 128] fp16; lse [n, Hq] fp32 is
-    written where given.  Rows that belong to no sequence are left as they are."""
-    rows, Hq = q.shape[0], q.shape[1] if q.dim() == 3 else 0
-    qs, ks, vs = _packed(q, "q"), _packed(k, "k", rows, cache.Hkv), _packed(v, "v", rows, cache.Hkv)
-    c, chunk = cache.paged_struct(), _chunk(cache, row_start, rows, max_rows)
-    if out is None:
-        out = torch.empty(rows, Hq, D, dtype=torch.float16, device=q.device)
-    os_ = _packed(out, "out", rows, Hq)
-    _need(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (rows, Hq)),
-          "lse has to be fp32 [rows, Hq]")
-    _on_device(cache.k_codes, q, k, v, row_start, out, lse)
-    if rows:
-        L = lib()
-        if n_split <= 0:
-            n_split = L.akvq_paged_default_splits(C.byref(c), Hq, min(max_rows, rows))
-        nws = L.akvq_paged_workspace_bytes(rows, Hq, n_split)
-        # of its own for every call: calls on two streams, or two captured graphs, share none
-        ws = torch.empty(nws, dtype=torch.uint8, device=q.device) if nws else None
-        _check(L.akvq_paged_attention(C.byref(c), C.byref(chunk), q.data_ptr(), qs, Hq, k.data_ptr(), ks, v.data_ptr(), vs, sm_scale,
-                                      out.data_ptr(), os_, _ptr(lse), n_split, _ptr(ws), nws, flags, _stream()), "akvq_paged_attention")
+    written where given.  Rows that belong to no sequence are left as they are.  The workspace is of its own for every call: calls on two
+    streams, or two captured graphs, share none."""
+    st, out = (_native or native()).paged_attention(cache, q, k, v, row_start, max_rows, sm_scale, n_split, flags, out, lse)
+    if st:
+        _check(st, "akvq_paged_attention")
     return out

@@ -3,9 +3,11 @@
 // is kept from one call for the next.  Through ctypes a step over a short context took longer on the host than on the GPU
 // (a descriptor of 14 fields, two allocations at 1.4 us, 18 converted arguments); one sequence of 640 tokens, 32 heads:
 // 11.1 -> 6.8 us a step, which is its time on the GPU.
+//   The calls for chunks likewise (below), with their checks of types, shapes and devices.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <algorithm>
 #include <cstring>
 
 #include <ATen/ATen.h>
@@ -23,7 +25,8 @@ constexpr int64_t kHeadDim = 128;
 // Attribute names of the cache object, made once.
 struct Names {
   PyObject *B, *Hkv, *G, *T_cap, *S_cap, *T_len, *k_codes, *v_codes, *k_meta, *v_meta, *k_sal, *v_sal, *sal_idx, *sal_cnt,
-      *fine_mask, *W, *k_win, *v_win, *workspace, *decode, *struct_, *window_struct;
+      *fine_mask, *W, *k_win, *v_win, *workspace, *decode, *struct_, *window_struct,
+      *page_rows, *n_pages, *max_pages, *max_len, *table, *seq_len, *paged_struct;
 } names;
 // What the package's own cache class describes itself with, and the types of the descriptions (plain_cache).
 struct Plain {
@@ -269,6 +272,289 @@ PyObject *decode_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- chunks: new rows of many sequences, packed token by token
+
+// plain_paged(paged_struct, paged_type, error): as plain_cache below, for the cache in pages; what these calls raise
+struct PlainPaged { PyObject *struct_ = nullptr, *type = nullptr, *error = nullptr; } paged;
+
+void need(bool ok, const char *what) {
+  if (ok) return;
+  PyErr_SetString(paged.error, what);
+  throw Failed();
+}
+void need(bool ok, const char *what, const char *why) {
+  if (ok) return;
+  PyErr_Format(paged.error, "%s%s", what, why);
+  throw Failed();
+}
+// The calls go to the current device's stream: a tensor of another device (or of the host) is refused.
+struct Here {
+  int device = -1;
+  void operator()(const at::Tensor &t) {
+    if (t.is_cuda() && device < 0) device = c10::hip::current_device();
+    need(t.is_cuda() && t.get_device() == device, "tensors have to be on the current device");
+  }
+  void *stream() const { return c10::hip::getCurrentHIPStream(device).stream(); }
+};
+// [rows, heads, 128] fp16 whose heads lie next to each other; returns the elements from row to row.  rows, heads: -1: any
+int64_t packed(const at::Tensor &t, const char *what, int64_t rows, int64_t heads) {
+  need(t.scalar_type() == at::kHalf && t.dim() == 3 && t.size(2) == kHeadDim, what, " has to be fp16 [rows, heads, 128]");
+  need((rows < 0 || t.size(0) == rows) && (heads < 0 || t.size(1) == heads), what, ": rows or heads do not fit");
+  need(t.stride(2) == 1 && (t.size(1) == 1 || t.stride(1) == kHeadDim), what, ": the heads of a row have to lie next to each other");
+  return t.size(0) > 1 ? t.stride(0) : t.size(1) * kHeadDim;
+}
+at::Tensor fresh(at::IntArrayRef shape, const at::Tensor &like) { return at::empty(shape, like.options().dtype(at::kHalf).requires_grad(false)); }
+
+akvq_axes axes_of(PyObject *o) {  // the description that RopeAxes holds
+  akvq_axes axes;
+  Py_buffer view;
+  if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw Failed();
+  const bool fits = view.len == (Py_ssize_t)sizeof(axes);
+  if (fits) std::memcpy(&axes, view.buf, sizeof(axes));
+  PyBuffer_Release(&view);
+  need(fits, "axes are described by something else");
+  return axes;
+}
+// positions [axes, rows], or [rows] for one axis; returns the elements from axis to axis
+int64_t positions(const at::Tensor &pos, int64_t rows, int axes) {
+  need(pos.scalar_type() == at::kInt && (pos.dim() == 1 || pos.dim() == 2), "positions have to be int32 [axes, rows]");
+  need(pos.size(-1) == rows && (pos.dim() == 2 ? pos.size(0) >= axes : axes == 1), "positions: one entry for every axis and row");
+  need(rows <= 1 || pos.stride(-1) == 1, "positions: the rows of an axis have to lie next to each other");
+  return pos.dim() == 2 && pos.size(0) > 1 ? pos.stride(0) : rows;
+}
+int count(int64_t n, const char *what) {
+  need(n >= 0 && n <= INT32_MAX, what, " does not fit 32 bits");
+  return (int)n;
+}
+
+// rope_axes(axes, pos, q, k, q_out, k_out, inverse) -> (status, (q_out, k_out))
+PyObject *rope_axes(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 7) {
+    PyErr_SetString(PyExc_TypeError, "rope_axes takes 7 arguments");
+    return nullptr;
+  }
+  try {
+    need(a[2] != Py_None || a[3] != Py_None, "neither q nor k");
+    const akvq_axes axes = axes_of(a[0]);
+    const at::Tensor &pos = tensor(a[1]);
+    const at::Tensor &lead = tensor(a[2] != Py_None ? a[2] : a[3]);
+    need(lead.dim() == 3, a[2] != Py_None ? "q" : "k", " has to be fp16 [rows, heads, 128]");
+    const int64_t rows = lead.size(0);
+    struct { const void *in = nullptr; void *out = nullptr; int64_t stride = 0, out_stride = 0; int heads = 0; } x[2];
+    at::Tensor outs[2];
+    static const char *const what[2] = {"q", "k"}, *const what_out[2] = {"q_out", "k_out"}, *const without[2] = {"q_out without q", "k_out without k"};
+    for (int i = 0; i < 2; ++i) {
+      if (a[2 + i] == Py_None) {
+        need(a[4 + i] == Py_None, without[i]);
+        continue;
+      }
+      const at::Tensor &t = tensor(a[2 + i]);
+      x[i].stride = packed(t, what[i], rows, -1);
+      outs[i] = a[4 + i] == Py_None ? fresh(t.sizes(), t) : tensor(a[4 + i]);
+      x[i].out_stride = packed(outs[i], what_out[i], rows, t.size(1));
+      x[i].in = t.data_ptr();
+      x[i].out = outs[i].data_ptr();
+      x[i].heads = count(t.size(1), "heads");
+    }
+    const int64_t pos_stride = positions(pos, rows, axes.n_axes);
+    Here here;
+    here(pos);
+    for (int i = 0; i < 2; ++i)
+      if (x[i].heads || a[2 + i] != Py_None) {
+        here(tensor(a[2 + i]));
+        here(outs[i]);
+      }
+    const int inverse = PyObject_IsTrue(a[6]);
+    if (inverse < 0) return nullptr;
+    int status = 0;
+    if (rows > 0) {
+      const int n_rows = count(rows, "rows");
+      void *const stream = here.stream();
+      const void *const at_pos = pos.data_ptr();
+      Py_BEGIN_ALLOW_THREADS
+      status = akvq_rope_axes(&axes, static_cast<const int32_t *>(at_pos), pos_stride, n_rows, x[0].in, x[0].stride, x[0].heads,
+                              x[1].in, x[1].stride, x[1].heads, x[0].out, x[0].out_stride, x[1].out, x[1].out_stride,
+                              inverse ? AKVQ_ROPE_INVERSE : 0, stream);
+      Py_END_ALLOW_THREADS
+    }
+    Held out[2];
+    for (int i = 0; i < 2; ++i) {
+      out[i].p = a[2 + i] == Py_None ? Py_NewRef(Py_None) : a[4 + i] != Py_None ? Py_NewRef(a[4 + i]) : THPVariable_Wrap(outs[i]);
+      if (!out[i].p) return nullptr;
+    }
+    return Py_BuildValue("i(OO)", status, out[0].p, out[1].p);
+  } catch (const Failed &) {
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+// rope_axes_table(axes, pos) -> (status, (cos, sin))
+PyObject *rope_axes_table(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 2) {
+    PyErr_SetString(PyExc_TypeError, "rope_axes_table takes 2 arguments");
+    return nullptr;
+  }
+  try {
+    const akvq_axes axes = axes_of(a[0]);
+    const at::Tensor &pos = tensor(a[1]);
+    need(pos.dim() == 1 || pos.dim() == 2, "positions have to be int32 [axes, rows]");
+    const int64_t rows = pos.size(-1), pos_stride = positions(pos, rows, axes.n_axes);
+    Here here;
+    here(pos);
+    const at::Tensor cos = fresh({rows, 64}, pos), sin = fresh({rows, 64}, pos);
+    int status = 0;
+    if (rows > 0)
+      status = akvq_rope_axes_table(&axes, static_cast<const int32_t *>(pos.data_ptr()), pos_stride, count(rows, "rows"), cos.data_ptr(),
+                                    sin.data_ptr(), here.stream());
+    Held c(THPVariable_Wrap(cos)), s(THPVariable_Wrap(sin));
+    if (!c.p || !s.p) return nullptr;
+    return Py_BuildValue("i(OO)", status, c.p, s.p);
+  } catch (const Failed &) {
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+// The cache's description, and the device of its pools.
+struct Pages {
+  akvq_paged c;
+  Held held;  // keeps what the pointers come from
+  Pages(PyObject *cache) {
+    if (described(cache, names.paged_struct, paged.struct_, paged.type, held, c)) {
+      need(held.p != Py_None, "paged_struct() of the cache returned None");
+      return;
+    }
+    struct { int32_t *to; PyObject *name; } ints[] = {
+        {&c.B, names.B}, {&c.Hkv, names.Hkv}, {&c.G, names.G}, {&c.page_rows, names.page_rows}, {&c.n_pages, names.n_pages},
+        {&c.max_pages, names.max_pages}, {&c.S_cap, names.S_cap}, {&c.max_len, names.max_len}};
+    for (auto &i : ints) *i.to = (int32_t)std::min<int64_t>(std::max<int64_t>(int_attr(cache, i.name), INT32_MIN), INT32_MAX);
+    c.k_codes = static_cast<uint32_t *>(ptr_attr(cache, names.k_codes));
+    c.v_codes = static_cast<uint32_t *>(ptr_attr(cache, names.v_codes));
+    c.k_meta = static_cast<uint32_t *>(ptr_attr(cache, names.k_meta));
+    c.v_meta = static_cast<uint32_t *>(ptr_attr(cache, names.v_meta));
+    c.k_sal = static_cast<uint16_t *>(ptr_attr(cache, names.k_sal));
+    c.v_sal = static_cast<uint16_t *>(ptr_attr(cache, names.v_sal));
+    c.sal_idx = static_cast<int32_t *>(ptr_attr(cache, names.sal_idx));
+    c.sal_cnt = static_cast<int32_t *>(ptr_attr(cache, names.sal_cnt));
+    c.table = static_cast<int32_t *>(ptr_attr(cache, names.table));
+    c.seq_len = static_cast<int32_t *>(ptr_attr(cache, names.seq_len));
+  }
+  // where the pools lie; the two tensors that the caller writes may have been put there by the caller
+  void on(PyObject *cache, Here &here) const {
+    Held k(PyObject_GetAttr(cache, names.k_codes));
+    if (!k.p) throw Failed();
+    here(tensor(k.p));
+    if (held.p) return;
+    Held t(PyObject_GetAttr(cache, names.table)), s(PyObject_GetAttr(cache, names.seq_len));
+    if (!t.p || !s.p) throw Failed();
+    const at::Tensor &table = tensor(t.p), &len = tensor(s.p);
+    need(table.scalar_type() == at::kInt && table.is_contiguous() && table.dim() == 2 && table.size(0) == c.B && table.size(1) == c.max_pages,
+         "table has to be int32 [sequences, max_pages]");
+    need(len.scalar_type() == at::kInt && len.is_contiguous() && len.dim() == 1 && len.size(0) == c.B, "seq_len has to be int32 [sequences]");
+    here(table);
+    here(len);
+  }
+};
+akvq_chunk chunk_of(const Pages &p, const at::Tensor &row_start, int64_t rows, PyObject *max_rows) {
+  need(row_start.scalar_type() == at::kInt && row_start.dim() == 1 && row_start.size(0) == p.c.B + 1 && row_start.is_contiguous(),
+       "row_start has to be int32 [sequences + 1]");
+  const long most = integer(max_rows);
+  need(most >= 0, "max_rows has to be at least 0");
+  return {static_cast<const int32_t *>(row_start.data_ptr()), count(rows, "rows"), (int32_t)std::min<long>(most, INT32_MAX)};
+}
+
+// paged_append(cache, k, v, row_start, max_rows, clip, flags) -> status
+PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 7) {
+    PyErr_SetString(PyExc_TypeError, "paged_append takes 7 arguments");
+    return nullptr;
+  }
+  try {
+    const Pages pages(a[0]);
+    const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]), &row_start = tensor(a[3]);
+    const int64_t ks = packed(k, "k", -1, pages.c.Hkv), rows = k.size(0), vs = packed(v, "v", rows, pages.c.Hkv);
+    const akvq_chunk chunk = chunk_of(pages, row_start, rows, a[4]);
+    Here here;
+    for (const at::Tensor *t : {&k, &v, &row_start}) here(*t);
+    pages.on(a[0], here);
+    const float clip = (float)number(a[5]);
+    const uint32_t flags = (uint32_t)integer(a[6]);
+    int status = 0;
+    if (rows > 0) {
+      void *const stream = here.stream();
+      const void *const k_at = k.data_ptr(), *const v_at = v.data_ptr();
+      Py_BEGIN_ALLOW_THREADS
+      status = akvq_paged_append(&pages.c, &chunk, k_at, ks, v_at, vs, clip, flags, stream);
+      Py_END_ALLOW_THREADS
+    }
+    return PyLong_FromLong(status);
+  } catch (const Failed &) {
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+// paged_attention(cache, q, k, v, row_start, max_rows, sm_scale, n_split, flags, out, lse) -> (status, out)
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 11) {
+    PyErr_SetString(PyExc_TypeError, "paged_attention takes 11 arguments");
+    return nullptr;
+  }
+  try {
+    const Pages pages(a[0]);
+    const at::Tensor &q = tensor(a[1]), &k = tensor(a[2]), &v = tensor(a[3]), &row_start = tensor(a[4]);
+    const int64_t qs = packed(q, "q", -1, -1), rows = q.size(0), ks = packed(k, "k", rows, pages.c.Hkv), vs = packed(v, "v", rows, pages.c.Hkv);
+    const int Hq = count(q.size(1), "heads");
+    const akvq_chunk chunk = chunk_of(pages, row_start, rows, a[5]);
+    const at::Tensor out = a[9] == Py_None ? fresh(q.sizes(), q) : tensor(a[9]);
+    const int64_t os = packed(out, "out", rows, Hq);
+    const at::Tensor lse = a[10] == Py_None ? at::Tensor() : tensor(a[10]);
+    need(!lse.defined() || (lse.scalar_type() == at::kFloat && lse.is_contiguous() && lse.dim() == 2 && lse.size(0) == rows && lse.size(1) == Hq),
+         "lse has to be fp32 [rows, Hq]");
+    Here here;
+    for (const at::Tensor *t : {&q, &k, &v, &row_start, &out}) here(*t);
+    if (lse.defined()) here(lse);
+    pages.on(a[0], here);
+    void *const lse_at = lse.defined() ? lse.data_ptr() : nullptr;
+    const float sm_scale = (float)number(a[6]);
+    const long asked = integer(a[7]);
+    const uint32_t flags = (uint32_t)integer(a[8]);
+    int status = 0;
+    if (rows > 0) {
+      const int n_split = asked > 0 ? (int)std::min<long>(asked, INT32_MAX)
+                                    : akvq_paged_default_splits(&pages.c, Hq, std::min(chunk.max_rows, chunk.n_rows));
+      const size_t bytes = akvq_paged_workspace_bytes(chunk.n_rows, Hq, n_split);
+      at::Tensor ws;  // of its own for every call: calls on two streams, or two captured graphs, share none
+      if (bytes) ws = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte).requires_grad(false));
+      void *const stream = here.stream(), *const ws_at = bytes ? ws.data_ptr() : nullptr, *const out_at = out.data_ptr();
+      const void *const q_at = q.data_ptr(), *const k_at = k.data_ptr(), *const v_at = v.data_ptr();
+      Py_BEGIN_ALLOW_THREADS
+      status = akvq_paged_attention(&pages.c, &chunk, q_at, qs, Hq, k_at, ks, v_at, vs, sm_scale, out_at, os,
+                                    static_cast<float *>(lse_at), n_split, ws_at, bytes, flags, stream);
+      Py_END_ALLOW_THREADS
+    }
+    Held o(a[9] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[9]));
+    if (!o.p) return nullptr;
+    return Py_BuildValue("iO", status, o.p);
+  } catch (const Failed &) {
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject *plain_paged(PyObject *, PyObject *args) {
+  PlainPaged p;
+  if (!PyArg_ParseTuple(args, "OOO", &p.struct_, &p.type, &p.error)) return nullptr;
+  for (PyObject *o : {p.struct_, p.type, p.error}) Py_INCREF(o);
+  paged = p;
+  Py_RETURN_NONE;
+}
+
 // plain_cache(struct, window_struct, cache_type, window_type): the functions of the package's own cache class, and the types
 // they return
 PyObject *plain_cache(PyObject *, PyObject *args) {
@@ -283,6 +569,11 @@ PyMethodDef methods[] = {
     {"plain_cache", plain_cache, METH_VARARGS, nullptr},
     {"decode_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_attention)), METH_FASTCALL, nullptr},
     {"decode_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(decode_step)), METH_FASTCALL, nullptr},
+    {"plain_paged", plain_paged, METH_VARARGS, nullptr},
+    {"rope_axes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rope_axes)), METH_FASTCALL, nullptr},
+    {"rope_axes_table", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rope_axes_table)), METH_FASTCALL, nullptr},
+    {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
+    {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attention)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_akvq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -295,7 +586,9 @@ PyMODINIT_FUNC PyInit__akvq_torch(void) {
       {&names.v_meta, "v_meta"}, {&names.k_sal, "k_sal"}, {&names.v_sal, "v_sal"}, {&names.sal_idx, "sal_idx"},
       {&names.sal_cnt, "sal_cnt"}, {&names.fine_mask, "fine_mask"}, {&names.W, "W"}, {&names.k_win, "k_win"},
       {&names.v_win, "v_win"}, {&names.workspace, "workspace"}, {&names.decode, "decode"},
-      {&names.struct_, "struct"}, {&names.window_struct, "window_struct"}};
+      {&names.struct_, "struct"}, {&names.window_struct, "window_struct"},
+      {&names.page_rows, "page_rows"}, {&names.n_pages, "n_pages"}, {&names.max_pages, "max_pages"}, {&names.max_len, "max_len"},
+      {&names.table, "table"}, {&names.seq_len, "seq_len"}, {&names.paged_struct, "paged_struct"}};
   for (auto &t : table)
     if ((*t.slot = PyUnicode_InternFromString(t.text)) == nullptr) return nullptr;
   return PyModule_Create(&module);
