@@ -365,10 +365,31 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int col = lane & (W - 1), g_lane = lane / W, n = lane & 15, p = kWide ? (lane >> 4) & 1 : 0;
   const int wk = MANY ? 0 : wave, wr = MANY ? wave : 0;
-  const int unit = blockIdx.x, b = unit / c.Hkv, head = unit % c.Hkv, R = a.Hq / c.Hkv, split = blockIdx.z;
+  const int head = blockIdx.x % c.Hkv, R = a.Hq / c.Hkv, split = blockIdx.z;
+  constexpr int kRows = (MANY ? NW : 1) * W;                     // of a workgroup
+  int b = blockIdx.x / c.Hkv, tile = gridDim.y - 1 - blockIdx.y;  // the rows that see most first
+  if constexpr (MANY) {
+    // One workgroup fills a CU, and there may be few more of them than CUs: the longest begin first, sequence by sequence.
+    if (c.B <= kWave) {
+      const int me = min(lane, c.B - 1);
+      const ChunkSpan mine = chunk_span(c.seq_len[me], c.row_start[me], c.row_start[me + 1], c);
+      const int tiles = lane < c.B ? (mine.rows * R + kRows - 1) / kRows : 0, keys = mine.len + mine.rows;
+      int begin = 0;  // of this lane's sequence in that order
+      for (int x = 0; x < c.B; ++x) {
+        const int other = __builtin_amdgcn_readlane(keys, x);
+        if (other > keys || (other == keys && x < lane)) begin += __builtin_amdgcn_readlane(tiles, x);
+      }
+      const int at = blockIdx.y * c.B + b;
+      const uint64_t here = __ballot(at >= begin && at < begin + tiles);
+      if (here == 0ull) return;  // whole workgroup
+      b = __builtin_ctzll(here);
+      tile = __builtin_amdgcn_readlane(begin + tiles, b) - 1 - at;
+    }
+  }
+  const int unit = b * c.Hkv + head;
   const ChunkSpan s = chunk_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
   const int rows = s.rows * R;                                  // of this unit: token by token, the heads of the group
-  const int wg_row = (gridDim.y - 1 - blockIdx.y) * ((MANY ? NW : 1) * W);  // first row of the workgroup: the rows that see most first
+  const int wg_row = tile * kRows;                              // first row of the workgroup
   if (wg_row >= rows) return;                                   // whole workgroup
   const int row0 = wg_row + wr * W;                             // first row of the wavefront
   const bool idle = row0 >= rows;                               // (of a workgroup whose wavefronts have rows of their own)
@@ -392,7 +413,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
     }
     wide = base;
   }
-  const int last_row = min(wg_row + (MANY ? NW : 1) * W, rows) - 1;
+  const int last_row = min(wg_row + kRows, rows) - 1;
   const int n_code = (s.len + 31) >> 5, n_wide = (wide + 31) >> 5, n_self = last_row / R / 32 + 1;
   // equal runs of the list, of a workgroup (many rows) or of a wavefront (few): a block of 16-bit rows counts as two of code rows
   const int parts = a.n_split * WK, wide_at = n_code, self_at = n_code + 2 * n_wide;
