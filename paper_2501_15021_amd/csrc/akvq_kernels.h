@@ -418,14 +418,22 @@ struct PagedAttentionArgs {
 hipError_t launch_paged_attention(const PagedAttentionArgs &a, int G, hipStream_t stream);
 constexpr int kPagedManyRows = 256;  // rows (tokens x heads of a group) of a workgroup that has many; its number is a grid dimension
 // How many splits of the keys, for units (sequences x KV heads) of at most `rows` rows (tokens x heads of a group) over at most `len`
-// cached rows: so many that as many workgroups as fit on a CU find work (three of up to 16 rows, else two; more than that and the merge
-// costs what the balance gains), with four blocks of 32 keys or more for each of them.
+// cached rows.  A workgroup's beginning and end and the merge cost as much as some blocks of 32 keys, so the CUs are filled once with few
+// blocks a workgroup, and further (as many as run together on a CU) only with many.  Measured, us: one row over 16384 cached rows of 32 units, 256
+// workgroups 21.1, 512 18.1, 768 20.1; over 32768 of 128 units, 512 103, 768 97; 32 rows over 8192 cached rows of 32 units, 256 21.3, 512 24.4;
+// over 32768, 256 40.4, 512 37.0; one row over 640 of 32 units, 2 splits 10.8, 5 splits 9.5.
 inline int paged_splits(long units, long rows, long len) {
   const long blocks = (len + 31) / 32, tiles = rows <= 16 ? 1 : rows <= 64 ? (rows + 31) / 32 : (rows + kPagedManyRows - 1) / kPagedManyRows;
-  long want = (rows <= 16 ? 768 : 512) / (units * tiles);
-  if (want > blocks / 4) want = blocks / 4;
-  if (want > 32) want = 32;
-  return (int)(want < 1 ? 1 : want);
+  long want = 1;
+  auto fill = [&](long workgroups, long least) {
+    long n = workgroups / (units * tiles);
+    if (n > blocks / least) n = blocks / least;
+    if (n > want) want = n;
+  };
+  if (rows <= 16) { fill(256, 4); fill(512, 8); fill(768, 64); }
+  else if (rows <= 64) { fill(256, 8); fill(512, 32); }
+  else fill(256, 8);
+  return (int)(want < 64 ? want : 64);
 }
 
 // status of a launch for the C ABI; keeps a failed launch's code for akvq_last_hip_error (akvq_api.hip)

@@ -32,6 +32,7 @@ namespace {
 constexpr int kDigits = 4;  // 3 or 4
 constexpr int kFewWaves = 4;   // of a workgroup that has few rows: they share them and deal the keys among them
 constexpr int kManyWaves = 8;  // of a workgroup that has many: each has its own, and all look at the same keys
+constexpr int kCus = 256;
 constexpr int kStageBlocks = 4;  // blocks of code rows that such a workgroup expands at a time, two wavefronts for each
 constexpr float kNoScore = -1.0e30f;   // score of a row that takes no part, reference of a column without scores
 constexpr float kRaiseAt = 15.0f;      // a score may exceed the reference by this (2^15 is the largest weight) ...
@@ -365,26 +366,31 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int col = lane & (W - 1), g_lane = lane / W, n = lane & 15, p = kWide ? (lane >> 4) & 1 : 0;
   const int wk = MANY ? 0 : wave, wr = MANY ? wave : 0;
-  const int head = blockIdx.x % c.Hkv, R = a.Hq / c.Hkv, split = blockIdx.z;
-  constexpr int kRows = (MANY ? NW : 1) * W;                     // of a workgroup
-  int b = blockIdx.x / c.Hkv, tile = gridDim.y - 1 - blockIdx.y;  // the rows that see most first
-  if constexpr (MANY) {
-    // One workgroup fills a CU, and there may be few more of them than CUs: the longest begin first, sequence by sequence.
-    if (c.B <= kWave) {
-      const int me = min(lane, c.B - 1);
-      const ChunkSpan mine = chunk_span(c.seq_len[me], c.row_start[me], c.row_start[me + 1], c);
-      const int tiles = lane < c.B ? (mine.rows * R + kRows - 1) / kRows : 0, keys = mine.len + mine.rows;
-      int begin = 0;  // of this lane's sequence in that order
-      for (int x = 0; x < c.B; ++x) {
-        const int other = __builtin_amdgcn_readlane(keys, x);
-        if (other > keys || (other == keys && x < lane)) begin += __builtin_amdgcn_readlane(tiles, x);
-      }
-      const int at = blockIdx.y * c.B + b;
-      const uint64_t here = __ballot(at >= begin && at < begin + tiles);
-      if (here == 0ull) return;  // whole workgroup
-      b = __builtin_ctzll(here);
-      tile = __builtin_amdgcn_readlane(begin + tiles, b) - 1 - at;
+  const int R = a.Hq / c.Hkv, split = blockIdx.z;
+  constexpr int kRows = (MANY ? NW : 1) * W;  // of a workgroup
+  int b = blockIdx.x / c.Hkv, head = blockIdx.x % c.Hkv, tile = gridDim.y - 1 - blockIdx.y;  // the rows that see most first
+  // Unequal sequences, where a CU gets few workgroups: which ones decides.  Where it holds one (many rows), the longest begin first; where it
+  // holds two or three, the first on every CU go from long to short, the second from short to long.
+  if (MANY ? c.B <= kWave : c.B <= kWave && gridDim.x > kCus && gridDim.y * gridDim.z == 1) {
+    const int me = min(lane, c.B - 1);
+    const ChunkSpan mine = chunk_span(c.seq_len[me], c.row_start[me], c.row_start[me + 1], c);
+    const int tiles = lane >= c.B ? 0 : MANY ? (mine.rows * R + kRows - 1) / kRows : 1, keys = mine.len + mine.rows;
+    int begin = 0;  // of this lane's sequence in that order, in tiles
+    for (int x = 0; x < c.B; ++x) {
+      const int other = __builtin_amdgcn_readlane(keys, x);
+      if (other > keys || (other == keys && x < lane)) begin += __builtin_amdgcn_readlane(tiles, x);
     }
+    int at = blockIdx.y * c.B + b;
+    if constexpr (!MANY) {
+      const int turn = blockIdx.x / kCus, last = min((int)gridDim.x, 2 * kCus) - 1;
+      const int place = turn == 1 ? last - (blockIdx.x - kCus) : blockIdx.x;
+      at = place / c.Hkv;
+      head = place - at * c.Hkv;
+    }
+    const uint64_t here = __ballot(at >= begin && at < begin + tiles);
+    if (here == 0ull) return;  // whole workgroup
+    b = __builtin_ctzll(here);
+    tile = __builtin_amdgcn_readlane(begin + tiles, b) - 1 - at;
   }
   const int unit = b * c.Hkv + head;
   const ChunkSpan s = chunk_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
