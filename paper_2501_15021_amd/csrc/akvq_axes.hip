@@ -24,21 +24,30 @@ __global__ __launch_bounds__(64 * kAxesWaves) void rope_axes_kernel(AxesArgs a) 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int row = blockIdx.x * kAxesWaves + wave;
   if (row >= a.n_rows) return;  // whole wavefront; no workgroup barrier below
+  const int o = lane & 7, first = blockIdx.y * a.heads_per_wave, end = min(first + a.heads_per_wave, a.Hq + a.Hkv);
+  // a head's row, or the last one's: asked for a head ahead, the first in front of the angle
+  auto source = [&](int h) {
+    h = min(h, a.Hq + a.Hkv - 1);
+    return (h >= a.Hq ? a.k + row * a.k_stride + (h - a.Hq) * kD : a.q + row * a.q_stride + h * kD) + 8 * o;
+  };
+  const uint16_t *src = source(first + (lane >> 3));
+  f16x8 next_lo = *reinterpret_cast<const f16x8 *>(src), next_hi = *reinterpret_cast<const f16x8 *>(src + 64);
   float c1, s1;
   pair_turn(a, lane, row, c1, s1);
   cos_lds[wave][lane] = c1;
   sin_lds[wave][lane] = a.inverse ? -s1 : s1;
   wave_lds_sync();
-  const int o = lane & 7;
   float c[8], s[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) { c[i] = cos_lds[wave][8 * o + i]; s[i] = sin_lds[wave][8 * o + i]; }
-  const int first = blockIdx.y * a.heads_per_wave, end = min(first + a.heads_per_wave, a.Hq + a.Hkv);
   for (int h = first + (lane >> 3); h < end; h += 8) {
-    const bool is_k = h >= a.Hq;
-    const uint16_t *src = is_k ? a.k + row * a.k_stride + (h - a.Hq) * kD : a.q + row * a.q_stride + h * kD;
-    uint16_t *dst = is_k ? a.k_out + row * a.k_out_stride + (h - a.Hq) * kD : a.q_out + row * a.q_out_stride + h * kD;
-    const f16x8 lo = *reinterpret_cast<const f16x8 *>(src + 8 * o), hi = *reinterpret_cast<const f16x8 *>(src + 64 + 8 * o);
+    uint16_t *dst = h >= a.Hq ? a.k_out + row * a.k_out_stride + (h - a.Hq) * kD : a.q_out + row * a.q_out_stride + h * kD;
+    const f16x8 lo = next_lo, hi = next_hi;
+    if (h + 8 < end) {
+      src = source(h + 8);
+      next_lo = *reinterpret_cast<const f16x8 *>(src);
+      next_hi = *reinterpret_cast<const f16x8 *>(src + 64);
+    }
     f16x8 lo2, hi2;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -65,7 +74,9 @@ __global__ __launch_bounds__(256) void rope_axes_table_kernel(AxesArgs a) {
 hipError_t launch_rope_axes(AxesArgs a, hipStream_t stream) {
   const unsigned blocks = ((unsigned)a.n_rows + kAxesWaves - 1) / kAxesWaves;
   const int heads = a.Hq + a.Hkv;
-  a.heads_per_wave = heads;
+  // few rows: their heads are dealt to as many wavefronts as fill the chip twice, eight heads (one round) each or more
+  const long long per = ((long long)a.n_rows * heads + 2047) / 2048;
+  a.heads_per_wave = per >= heads ? heads : (int)((per + 7) / 8 * 8);
   const unsigned parts = (heads + a.heads_per_wave - 1) / a.heads_per_wave;
   rope_axes_kernel<<<dim3(blocks, parts), dim3(64 * kAxesWaves), 0, stream>>>(a);
   return hipGetLastError();
