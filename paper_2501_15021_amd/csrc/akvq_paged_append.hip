@@ -202,9 +202,69 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   else paged_append_body<G, 1>(a, slot_of);
 }
 
+// A row's place in its list of salient rows as RowSlot, but sampled: lists of pages are as long as the prompts' text.
+struct SampledSlot : RowSlot {
+  using RowSlot::RowSlot;
+  __device__ __forceinline__ int find(int t) const {
+    const int n = min(max(cnt, 0), cap);
+    int base = 0, e = first_entry;
+    if (n > kWave) {
+      for (int span = n; span > 1;) {  // the row's entry, if there is one, is in [base, base + span)
+        const int step = (span + 63) >> 6, at = base + lane * step;
+        e = lane * step < span && at < n ? sidx[at] : 0x7FFFFFFF;
+        base += max(__popcll(__ballot(e <= t)) - 1, 0) * step;
+        span = step;
+      }
+      return __ballot(e == t) != 0ull ? base : -1;
+    }
+    const unsigned long long hit = __ballot(lane < n && e == t);
+    return hit != 0ull ? __builtin_ctzll(hit) : -1;
+  }
+};
+
+// One generated token of every sequence: a wavefront a row and tensor (append_row_wave), the block's place in its page put under the place
+// that the row would have in a plane of its own.  Latency bound.
+template <int G>
+__global__ __launch_bounds__(64) void paged_append_row_kernel(PagedAppendArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t code_lds[kD];
+  __shared__ __attribute__((aligned(16))) uint16_t row_lds[kD];
+  const PagedArgs &c = a.c;
+  const int unit = blockIdx.x, b = unit / c.Hkv, head = unit % c.Hkv;
+  const ChunkSpan s = chunk_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
+  if (s.rows == 0 || s.len >= c.row_cap) return;
+  const int page = c.table[(size_t)b * c.max_pages + (s.len >> c.page_shift)];
+  if (page < 0 || page >= c.n_pages) return;
+  const int t0 = s.len & ~(kTokBlock - 1);
+  const long long row0 = ((((long long)page * c.Hkv + head) << c.page_shift) + (t0 & ((1 << c.page_shift) - 1))) - t0;
+  QuantArgs q = {};
+  q.k_new = a.k + s.first * a.k_stride + (head - unit) * kD;  // (append_row_wave adds what the unit's row and planes lie behind)
+  q.v_new = a.v + s.first * a.v_stride + (head - unit) * kD;
+  q.k_codes = c.k_codes + row0 * (kBlockWords / kTokBlock);
+  q.v_codes = c.v_codes + row0 * (kBlockWords / kTokBlock);
+  q.k_meta = c.k_meta + row0 * (kD / G);
+  q.v_meta = c.v_meta + row0 * (kD / G);
+  q.k_sal = c.k_sal;
+  q.v_sal = c.v_sal;
+  q.sal_idx = c.sal_idx;
+  q.sal_cnt = c.sal_cnt;
+  q.Hkv = c.Hkv;
+  q.S_cap = c.S_cap;
+  q.T_len = s.len;
+  q.clip = a.clip;
+  q.rotate_k = a.rotate_k;
+  q.rotate_v = a.rotate_v;
+  append_row_wave<G, SampledSlot>(q, unit, blockIdx.y, threadIdx.x, code_lds, row_lds);
+}
+
 }  // namespace
 
 hipError_t launch_paged_append(const PagedAppendArgs &a, int G, hipStream_t stream) {
+  if (a.c.max_rows == 1) {
+    const dim3 grid(a.c.B * a.c.Hkv, 2);
+    if (G == 128) paged_append_row_kernel<128><<<grid, dim3(64), 0, stream>>>(a);
+    else paged_append_row_kernel<64><<<grid, dim3(64), 0, stream>>>(a);
+    return hipGetLastError();
+  }
   const int blocks = (a.c.max_rows + 30) / kTokBlock + 1;  // that max_rows rows can touch, wherever they start
   const dim3 grid((blocks + 3) / 4, a.c.B * a.c.Hkv, 2), block(256);
   if (G == 128) paged_append_kernel<128><<<grid, block, 0, stream>>>(a);

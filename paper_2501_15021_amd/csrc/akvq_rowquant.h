@@ -104,9 +104,27 @@ __device__ __forceinline__ float wave_max_all(float v) {
   return v;
 }
 
+// Where a row stands in the ascending list of (batch, kv-head) bh's salient rows (-1: nowhere), looked for 64 entries at a time.
+struct RowSlot {
+  const int32_t *sidx;
+  int cnt, cap, first_entry, lane;
+  __device__ __forceinline__ RowSlot(const QuantArgs &a, int bh, int lane_)
+      : sidx(a.sal_idx + (size_t)bh * a.S_cap), cnt(a.sal_cnt[bh]), cap(a.S_cap), first_entry(sidx[lane_]), lane(lane_) {}  // S_cap >= 64: asked for together with the count instead of after it
+  __device__ __forceinline__ int find(int t) const {
+    const int n = min(max(cnt, 0), cap);
+    int slot = -1;
+    for (int base = 0; base < n; base += kWave) {
+      const int e = base + lane < n ? (base == 0 ? first_entry : sidx[base + lane]) : -1;
+      const unsigned long long hit = __ballot(e == t);
+      if (hit != 0ull) slot = base + __builtin_ctzll(hit);
+    }
+    return slot;
+  }
+};
+
 // One wavefront writes row a.T_len of (batch, kv-head) bh of one tensor (0 = K, 1 = V); code_lds (128 bytes) and
 // row_lds (128 x 16 bit) are scratch of this wavefront alone.
-template <int G>
+template <int G, typename Slot = RowSlot>
 __device__ __forceinline__ void append_row_wave(const QuantArgs &a, int bh, int tensor, int lane, uint8_t *code_lds,
                                                 uint16_t *row_lds) {
   constexpr int NG = kD / G;
@@ -116,9 +134,7 @@ __device__ __forceinline__ void append_row_wave(const QuantArgs &a, int bh, int 
   const float kappa = rotate ? inv_sqrt128() : 1.0f;
 
   // everything that has to come from memory is requested first
-  const int32_t *sidx = a.sal_idx + (size_t)bh * a.S_cap;
-  int cnt = a.sal_cnt[bh];
-  const int first_entry = sidx[lane];  // S_cap >= 64: asked for together with the count instead of after it
+  const Slot list(a, bh, lane);
   const uint16_t *row = (tensor == 0 ? a.k_new : a.v_new) + (size_t)bh * kD;
   float x0 = half_bits_to_float(row[lane]), x1 = half_bits_to_float(row[lane + 64]);
   const size_t blk_word = ((size_t)bh * (a.T_cap / kTokBlock) + blk) * kBlockWords;
@@ -137,13 +153,7 @@ __device__ __forceinline__ void append_row_wave(const QuantArgs &a, int bh, int 
   }
 
   // is the row listed as salient, and at which rank?
-  cnt = min(max(cnt, 0), a.S_cap);
-  int slot = -1;
-  for (int base = 0; base < cnt; base += kWave) {
-    const int e = base + lane < cnt ? (base == 0 ? first_entry : sidx[base + lane]) : -1;
-    const unsigned long long hit = __ballot(e == t);
-    if (hit != 0ull) slot = base + __builtin_ctzll(hit);
-  }
+  const int slot = list.find(t);
 
   if (rotate) {
 #pragma unroll
