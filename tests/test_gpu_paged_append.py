@@ -54,6 +54,43 @@ def test_like_the_contiguous_write_path(lens, rows, Hkv, page_rows, G):
     _check(s)
 
 
+@pytest.mark.parametrize("G", [128, 64])
+@pytest.mark.parametrize("flags", [0, akvq.K_PREROTATED | akvq.V_PREROTATED])
+def test_single_rows(G, flags):
+    """One row a sequence at every kind of place in a block and a page, none for some; rows that are salient and rows that are not."""
+    lens = [0, 1, 3, 15, 16, 17, 31, 32, 47, 63, 64, 95, 127, 200]
+    s = Sequences(lens, [0 if i in (4, 9) else 1 for i in range(len(lens))], 3, G, 32, salient=[0, 1, 15, 31, 33, 64, 95, 200], seed=G + flags)
+    _scramble(s)
+    _check(s, flags=flags)
+
+
+@pytest.mark.parametrize("count,step", [(1, 1), (64, 2), (65, 1), (66, 3), (1000, 1), (4097, 2), (6000, 1)])
+def test_single_rows_and_long_salient_lists(count, step):
+    """The row's entry first, last, in the middle of the list, just missing from it, and behind all of it."""
+    lens = [0, (count - 1) * step, count // 2 * step, count // 2 * step + 1, count * step + 5]
+    s = Sequences(lens, [1] * 5, 2, 128, salient=range(0, count * step, step), seed=count, S_cap=(count + 63) // 64 * 64)
+    for b in range(5):  # final for rows that are still to come, as they are while a prompt is written
+        s.cache.sal_idx[b, :, :count] = torch.arange(0, count * step, step, dtype=torch.int32, device="cuda")
+        s.cache.counts()[b] = count
+    _scramble(s)
+    _check(s)
+
+
+def test_single_rows_without_a_page_and_behind_the_table_are_dropped():
+    s = Sequences([63, 64, 40], [1, 1, 1], 2, 128)
+    p = s.cache
+    p.table[1, 1] = -1
+    p.table[2, 0] = p.n_pages
+    p.max_len = p.max_pages * p.page_rows
+    _scramble(s)
+    p.seq_len.copy_(torch.tensor([p.max_len, 64, 40], dtype=torch.int32))  # the first is full
+    before = {name: getattr(p, name).clone() for name in POOLS + ("k_sal", "v_sal")}
+    akvq.paged_append(p, s.k, s.v, s.row_start, 1, 0.8)
+    torch.cuda.synchronize()
+    for name, old in before.items():
+        assert torch.equal(getattr(p, name), old), name
+
+
 @pytest.mark.parametrize("flags", [akvq.K_PREROTATED, akvq.V_PREROTATED, akvq.K_PREROTATED | akvq.V_PREROTATED])
 def test_rows_that_arrive_rotated(flags):
     s = Sequences([9, 40], [50, 7], 3, 64, salient=range(0, 60, 7))

@@ -33,6 +33,28 @@ def test_against_the_formula(lens, rows, Hq, Hkv, page_rows, G):
         check_attention(s, out, lse, SM, f"n_split {n_split}")
 
 
+@pytest.mark.parametrize("lens,rows,Hq,Hkv", [
+    ([70, 3, 0, 200, 33, 64, 1, 150, 90], [1, 1, 1, 1, 0, 1, 1, 1, 1], 32, 32),                 # more units than CUs: paired on them
+    ([(37 * b) % 101 for b in range(65)], [b % 2 for b in range(65)], 8, 8),                    # more sequences than lanes
+    ([5, 300, 0, 300, 64, 20], [70, 65, 129, 1, 0, 300], 2, 2),                                 # unequal chunks, the longest first
+    ([(37 * b) % 101 for b in range(66)], [66 if b % 8 == 0 else b % 3 for b in range(66)], 1, 1)])
+def test_the_order_of_unequal_sequences(lens, rows, Hq, Hkv):
+    """Which sequence a workgroup takes depends on all lengths: every row is still written once, with its own result."""
+    s = Sequences(lens, rows, Hkv, 128, 32, Hq=Hq, salient=SALIENT, seed=len(lens)).fill_pages()
+    for n_split in (1, 2):
+        out, lse = _run(s, n_split)
+        check_attention(s, out, lse, SM, f"n_split {n_split}")
+
+
+@pytest.mark.parametrize("n_split", [16, 17, 33, 64, 130])
+@pytest.mark.parametrize("rows", [1, 20, 70])
+def test_many_splits(n_split, rows):
+    """More splits than the merge takes at a time, and more than there are blocks."""
+    s = Sequences([700, 20], [rows, 1], 2, 64, Hq=4, salient=SALIENT, seed=n_split).fill_pages()
+    out, lse = _run(s, n_split)
+    check_attention(s, out, lse, SM)
+
+
 @pytest.mark.parametrize("salient", [[], range(0, 500), range(1, 500, 2), [499]])
 @pytest.mark.parametrize("rows", [1, 40, 150])
 def test_few_and_many_16_bit_rows(salient, rows):
