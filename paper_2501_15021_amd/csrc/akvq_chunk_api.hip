@@ -147,7 +147,7 @@ size_t akvq_paged_workspace_bytes(int n_rows, int Hq, int n_split) {
 int akvq_paged_default_splits(const akvq_paged *c, int Hq, int max_rows) {
   if (check_paged_shape(c) != AKVQ_OK || Hq <= 0 || Hq % c->Hkv != 0 || max_rows <= 0) return 1;
   const int64_t cap = (int64_t)c->max_pages * c->page_rows;
-  return akvq::paged_splits((long)c->B * c->Hkv, (long)max_rows * (Hq / c->Hkv), (long)(c->max_len < cap ? c->max_len : cap));
+  return akvq::paged_splits((long)c->B * c->Hkv, max_rows, Hq / c->Hkv, (long)(c->max_len < cap ? c->max_len : cap));
 }
 
 int akvq_paged_attention(const akvq_paged *c, const akvq_chunk *rows, const void *q, int64_t q_stride, int Hq, const void *k,

@@ -499,7 +499,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
   };
 
   // against 16-bit rows the query is two bfloat16 terms, 16 bits
-  // up to 16 rows: the wavefronts' sums over cached rows are merged before they are rotated back, once
+  // tiles of 16: the wavefronts' sums over cached rows are merged before they are rotated back, once
   constexpr bool kMergeFirst = W == 16;
   u32x4 q_hi[NC], q_lo[NC];
   auto split_query = [&](const float (&x)[8 * NC]) {
@@ -1326,8 +1326,10 @@ void launch_variant(const PagedAttentionArgs &a, int rows, hipStream_t stream) {
   const int units = a.c.B * a.c.Hkv;
   auto grid = [&](int per) { return dim3(units, (rows + per - 1) / per, a.n_split); };
   constexpr int kFew = 64 * kFewWaves, kMany = 64 * kManyWaves;
-  if (rows <= 16) paged_attention_kernel<G, 16, false><<<grid(16), kFew, 0, stream>>>(a);
-  else if (rows <= 64) paged_attention_kernel<G, 32, false><<<grid(32), kFew, 0, stream>>>(a);
+  static_assert(kPagedManyRows == 32 * kManyWaves);
+  const int per = paged_tile_rows(units, a.c.max_rows, a.Hq / a.c.Hkv, a.c.max_len);
+  if (per == 16) paged_attention_kernel<G, 16, false><<<grid(16), kFew, 0, stream>>>(a);
+  else if (per == 32) paged_attention_kernel<G, 32, false><<<grid(32), kFew, 0, stream>>>(a);
   else paged_attention_kernel<G, 32, true><<<grid(kPagedManyRows), kMany, 0, stream>>>(a);
 }
 

@@ -46,6 +46,17 @@ def test_the_order_of_unequal_sequences(lens, rows, Hq, Hkv):
         check_attention(s, out, lse, SM, f"n_split {n_split}")
 
 
+@pytest.mark.parametrize("lens,rows,Hq,Hkv", [
+    ([100, 1000], [17, 32], 2, 2), ([40, 0, 333], [4, 3, 1], 28, 4),           # two tiles of 16 rows
+    ([0, 500], [300, 260], 3, 3), ([0], [1100], 2, 1), ([64, 3], [70, 513], 8, 1),  # tiles of 32 of long chunks
+    ([17000], [40], 4, 1), ([5000, 0, 200], [600, 2900, 1], 1, 1)])             # tiles of 256
+def test_tiles_of_every_size(lens, rows, Hq, Hkv):
+    s = Sequences(lens, rows, Hkv, 64, 64, Hq=Hq, salient=SALIENT, seed=sum(rows)).fill_pages()
+    for n_split in (0, 1, 3):
+        out, lse = _run(s, n_split)
+        check_attention(s, out, lse, SM, f"n_split {n_split}")
+
+
 @pytest.mark.parametrize("n_split", [16, 17, 33, 64, 130])
 @pytest.mark.parametrize("rows", [1, 20, 70])
 def test_many_splits(n_split, rows):
