@@ -358,14 +358,14 @@ int akvq_paged_append(const akvq_paged *c, const akvq_chunk *rows, const void *k
  *   chunk's rows j <= i of the same sequence, which count as they arrive (binary16), whether or not akvq_paged_append has already
  *   stored them behind seq_len.  One row a sequence is the decode step of a batch of unequal lengths; nothing cached is a first chunk.
  *   q, k, v: post-RoPE, un-rotated.  out: [n_rows][Hq][128] binary16, rows out_stride elements apart.  lse_out: optional, [n_rows][Hq]
- *   fp32.  Hq / Hkv at most 8, max_rows * Hq / Hkv below 2^24 - 256.  fp32 scores, sums and accumulators; the cached rows' queries as integers of 20 bits (16 against
- *   16-bit rows), weights of 11 bits (16 for the 16-bit rows).
+ *   fp32.  Hq / Hkv at most 8, max_rows * Hq / Hkv below 2^24 - 256.  fp32 scores, sums and accumulators; the cached rows' queries as
+ *   integers of 20 bits (16 against 16-bit rows), weights of 11 bits (16 for the 16-bit rows).
  *   Rows listed as salient are read from the overlay whatever their page.  NaN or infinity in a sequence's own rows gives
  *   unspecified values for that sequence and KV head, never for others.
  *   flags: AKVQ_Q_PREROTATED (q and k arrive rotated), AKVQ_OUT_ROTATED (the chunk's v rows arrive rotated, out is left rotated).
- *   n_split <= 0 lets the library choose, akvq_paged_default_splits() at most; larger than 1024 is refused.  workspace: device,
- *   akvq_paged_workspace_bytes() bytes of n_split, or of that maximum (0 bytes, and NULL, for one split); calls that may overlap need
- *   one each.  out may not overlap q, k or v.  n_rows = 0 does nothing.
+ *   n_split <= 0 lets the library choose, akvq_paged_default_splits() of the call's max_rows; larger than 1024 is refused.  workspace:
+ *   device, akvq_paged_workspace_bytes() bytes of n_split, or of that choice (0 bytes, and NULL, for one split); calls that may overlap
+ *   need one each.  out may not overlap q, k or v.  n_rows = 0 does nothing.
  */
 size_t akvq_paged_workspace_bytes(int n_rows, int Hq, int n_split);
 int akvq_paged_default_splits(const akvq_paged *c, int Hq, int max_rows);

@@ -4,6 +4,8 @@
 // pair i once for all heads (a 64-bit product, whose whole turns are dropped before 32 bits hold it: a 32-bit angle would be off by
 // 2^-24 of itself, 6e-3 at position 100000) and leaves its sine and cosine in LDS, from where lane (h, o) takes those of pairs
 // 8o .. 8o + 7 for every eighth head: two 128-bit loads and stores a head, 128 contiguous bytes for eight lanes.
+//   Measured: 8 x 8191 rows of 32 heads 131 us, 5.4 TB/s (a large copy: 5.47); sixteen rows of 64 heads 2.3 us, a launch and one round
+// trip to memory (4.4 with a wavefront a row, and the first head behind the angle).
 #include "akvq_device.h"
 #include "akvq_kernels.h"
 

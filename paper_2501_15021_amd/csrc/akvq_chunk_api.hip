@@ -166,7 +166,7 @@ int akvq_paged_attention(const akvq_paged *c, const akvq_chunk *rows, const void
       check_rows(out, out_stride, Hq) != AKVQ_OK)
     return AKVQ_ERR_INVALID_ARG;
   if (lse_out && !aligned(lse_out, 4)) return AKVQ_ERR_INVALID_ARG;
-  if (n_split <= 0) n_split = akvq_paged_default_splits(c, Hq, a.c.max_rows);
+  if (n_split <= 0) n_split = akvq_paged_default_splits(c, Hq, rows->max_rows);  // (of the caller's bound: what its workspace is sized for)
   if (n_split > 1) {
     if (!workspace || !aligned(workspace, 16)) return AKVQ_ERR_INVALID_ARG;
     if (workspace_bytes < akvq_paged_workspace_bytes(rows->n_rows, Hq, n_split)) return AKVQ_ERR_WORKSPACE;

@@ -19,10 +19,17 @@
 // 4^ii / scale, and zero-points are summed with the rounded weights.
 //   Weights are binary16 (half a step is 2^-12 of a weight), relative to a reference that keeps the largest between 2^7 and 2^15: a
 // weight below 2^-21 of its row's largest loses bits, one below 2^-31 all of them.  Scores, references, sums and accumulators are 32-bit.
-//   Bound: many rows by the issue of vector and matrix instructions together, which share a SIMD's time (measured: a 32x32 product keeps
-// the vector unit for 15 of its 33 cycles, a 16x16 one for 12 of 19, a vector instruction takes 3, an exponential 9).  Tiles of 32 x 32
-// and two wavefronts a SIMD follow from that.  Few rows (up to 16 of a unit: one generated token) are bound by the cache's stream and take
-// tiles of 16 x 16.
+//   Rows of a unit (a sequence's tokens times the heads of a KV head) come in tiles of 16 or 32 whose four wavefronts share the rows and deal
+// the keys among them, or of 256, 32 for each of eight wavefronts that look at the same keys (paged_tile_rows says which, and what it measured).
+//   Tiles of 256 are bound by the issue of vector and matrix instructions together, which share a SIMD's time (measured: a 32x32 product keeps
+// the vector unit for 15 of its 33 cycles, a 16x16 one for 12 of 19, a vector instruction takes 3 to 4, an exponential 9), and by the power that
+// matrix instructions may take (the 17 products of a block alone, on random data, take 0.9 ms of what follows).  So every block is expanded once
+// for all eight.  4 x 2048 rows of 32 heads over 8192 cached ones: 1.25-1.3 ms, 960-1000 TFLOP/s of what the formula takes (a 16-bit
+// matrix product of 8192 x 8192 x 8192: 1268); first chunks of 4096, which LDS reads bind as much, 0.28 ms, 780.
+//   Tiles of 16 and 32 read the cache with what their wavefronts have under way.  One row of 4 heads over 32768 rows of 128 units (G = 64):
+// 94-97 us, 3.6 TB/s, where vector instructions take 63 % of the time and matrix instructions 27; one row over 2048 to 4096 rows of 512 units 36 us, 3.2
+// TB/s, 13 of it before the first block and behind the last: two wavefronts a SIMD, 42 and 14 %.  One row over 640 of 32 units: 8.5 us and 2.8
+// for the merge, a chain of memory round trips.
 #include "akvq_device.h"
 #include "akvq_kernels.h"
 

@@ -1,4 +1,5 @@
 """Attention of a chunk over pages and over itself (akvq_paged_attention) against the formula in 64 bits on what the pages hold."""
+import ctypes as C
 import math
 
 import pytest
@@ -55,6 +56,22 @@ def test_tiles_of_every_size(lens, rows, Hq, Hkv):
     for n_split in (0, 1, 3):
         out, lse = _run(s, n_split)
         check_attention(s, out, lse, SM, f"n_split {n_split}")
+
+
+def test_default_splits_of_the_callers_bound():
+    """The library's choice is that of the max_rows it is given, also where fewer rows come: a workspace of that size serves them."""
+    s = Sequences([3000, 40], [1, 0], 2, 128, Hq=4, salient=SALIENT, seed=2).fill_pages()
+    L, c = akvq.lib(), s.cache.paged_struct()
+    for max_rows in (1, 9, 200, 5000):
+        n = L.akvq_paged_default_splits(C.byref(c), 4, max_rows)
+        nws = L.akvq_paged_workspace_bytes(s.n, 4, n)
+        ws = torch.empty(max(nws, 16), dtype=torch.uint8, device="cuda")
+        out = torch.empty(s.n, 4, 128, dtype=torch.float16, device="cuda")
+        chunk = akvq.akvq_chunk(s.row_start.data_ptr(), s.n, max_rows)
+        assert L.akvq_paged_attention(C.byref(c), C.byref(chunk), s.q.data_ptr(), s.q.stride(0), 4, s.k.data_ptr(), s.k.stride(0), s.v.data_ptr(),
+                                      s.v.stride(0), SM, out.data_ptr(), 512, None, 0, ws.data_ptr(), nws, 0, None) == 0
+        torch.cuda.synchronize()
+        check_attention(s, out, None, SM, f"max_rows {max_rows}")
 
 
 @pytest.mark.parametrize("n_split", [16, 17, 33, 64, 130])
