@@ -1,5 +1,5 @@
-"""Thin binding of libakvq.so (C ABI in include/akvq.h): ctypes, and for the two decode calls the native module
-_akvq_torch (csrc/akvq_torch.cpp), which marshals the same arguments.
+"""Thin binding of libakvq.so (C ABI in include/akvq.h): ctypes, and for the two decode calls and those for
+chunks the native module _akvq_torch (csrc/akvq_torch.cpp), which marshals the same arguments.
 
 Argument marshalling only: torch supplies device memory and the current stream; every step of the
 method runs inside the library's HIP kernels.  There is no fallback: if the library is missing or a

@@ -275,7 +275,7 @@ PyObject *decode_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // ---- chunks: new rows of many sequences, packed token by token
 
 // plain_paged(paged_struct, paged_type, error): as plain_cache below, for the cache in pages; what these calls raise
-struct PlainPaged { PyObject *struct_ = nullptr, *type = nullptr, *error = nullptr; } paged;
+struct PlainPaged { PyObject *struct_ = nullptr, *type = nullptr, *error = PyExc_RuntimeError; } paged;
 
 void need(bool ok, const char *what) {
   if (ok) return;
@@ -528,7 +528,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (rows > 0) {
       const int n_split = asked > 0 ? (int)std::min<long>(asked, INT32_MAX)
                                     : akvq_paged_default_splits(&pages.c, Hq, std::min(chunk.max_rows, chunk.n_rows));
-      const size_t bytes = akvq_paged_workspace_bytes(chunk.n_rows, Hq, n_split);
+      const size_t bytes = n_split <= 1024 ? akvq_paged_workspace_bytes(chunk.n_rows, Hq, n_split) : 0;  // (more is refused by the call)
       at::Tensor ws;  // of its own for every call: calls on two streams, or two captured graphs, share none
       if (bytes) ws = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte).requires_grad(false));
       void *const stream = here.stream(), *const ws_at = bytes ? ws.data_ptr() : nullptr, *const out_at = out.data_ptr();

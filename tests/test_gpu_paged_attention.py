@@ -284,3 +284,63 @@ def test_the_same_again_and_on_two_streams():
     torch.cuda.synchronize()
     for i, out in enumerate(got):
         assert torch.equal(out, want[i % 2][0])
+
+
+def test_tables_and_caches_that_the_caller_made():
+    """The two tensors that the caller may replace are looked at; a cache that describes itself is asked."""
+    s = Sequences([70, 3], [2, 1], 2, 128, Hq=4).fill_pages()
+    want, _ = _run(s, 2)
+    good = {n: getattr(s.cache, n) for n in ("table", "seq_len")}
+    for name, bad, why in [("table", good["table"].long(), "table"), ("table", good["table"][:1], "table"), ("table", good["table"].cpu(), "current device"),
+                           ("seq_len", good["seq_len"].long(), "seq_len"), ("seq_len", good["seq_len"][:1], "seq_len"),
+                           ("seq_len", good["seq_len"].cpu(), "current device"), ("table", torch.stack((good["table"],) * 2, 2)[:, :, 0], "table")]:
+        setattr(s.cache, name, bad)
+        for call in (lambda: _run(s), lambda: akvq.paged_append(s.cache, s.k, s.v, s.row_start, s.max_rows, 0.8)):
+            with pytest.raises(akvq.AkvqError, match=why):
+                call()
+        setattr(s.cache, name, good[name])
+    with pytest.raises(akvq.AkvqError):
+        _run(s, 1025)
+
+    class Own(akvq.PagedCache):
+        def paged_struct(self):
+            asked.append(self)
+            return super().paged_struct()
+
+    asked = []
+    s.cache.__class__ = Own
+    assert torch.equal(_run(s, 2)[0], want) and asked == [s.cache]
+    s.cache.paged_struct = lambda: None
+    with pytest.raises(akvq.AkvqError, match="None"):
+        _run(s)
+    s.cache.paged_struct = lambda: s.cache.struct()  # of a contiguous cache
+    with pytest.raises(TypeError):
+        _run(s)
+
+
+@pytest.mark.parametrize("rows,Hq,Hkv", [([1] * 9, 32, 32), ([20, 0, 32], 4, 2), ([300, 70, 0], 2, 1), ([2100, 1, 900], 1, 1)])
+def test_captured_while_lengths_and_pages_change(rows, Hq, Hkv):
+    """One capture of every tile size, replayed over other lengths, other pages and another share of the rows, each time against an eager call."""
+    lens = [(61 * b + 30) % 200 + 60 for b in range(len(rows))]
+    s = Sequences(lens, rows, Hkv, 128, 32, Hq=Hq, salient=SALIENT, seed=sum(rows)).fill_pages()
+    table, starts = s.cache.table.clone(), s.row_start.clone()
+    out, want = torch.zeros(s.n, Hq, 128, dtype=torch.float16, device="cuda"), torch.zeros(s.n, Hq, 128, dtype=torch.float16, device="cuda")
+
+    def call(x):
+        akvq.paged_attention(s.cache, s.q, s.k, s.v, s.row_start, s.max_rows, SM, out=x)
+
+    call(want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for step in range(4):
+        s.cache.seq_len.copy_(torch.tensor([(t * (step + 1)) % (t + 1) for t in lens], dtype=torch.int32))
+        s.cache.table.copy_(table if step % 2 == 0 else table.roll(1, 1))
+        s.row_start.copy_(starts if step < 2 else starts // 2)
+        out.fill_(5)
+        want.fill_(5)
+        graph.replay()
+        call(want)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), step
