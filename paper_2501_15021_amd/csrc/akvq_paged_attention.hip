@@ -252,6 +252,8 @@ __device__ __forceinline__ MetaWords<NG> load_meta(const uint32_t *at) {
     return {{*at}};
   }
 }
+// Scales of 0, which only rows have that were never written, count as the smallest that binary16 holds: their reciprocal is needed.
+constexpr float kLeastScale = 5.9604645e-8f;  // 2^-24
 // A row's scales and zero-points; one that takes no part has a scale of 1 and nothing else
 template <int NG>
 struct RowMeta {
@@ -261,7 +263,7 @@ struct RowMeta {
     part = there && (m.w[0] & 0x8000u) == 0u;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      scale[g] = part ? half_bits_to_float(m.w[g] & 0x7FFFu) : 1.0f;
+      scale[g] = part ? fmaxf(half_bits_to_float(m.w[g] & 0x7FFFu), kLeastScale) : 1.0f;
       zero[g] = part ? (float)((int)m.w[g] >> 16) : 0.0f;
     }
     top = NG == 2 && value ? fmaxf(scale[0], scale[NG - 1]) : scale[0];  // (keys: the first group's)
@@ -821,7 +823,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
           if constexpr (NG == 2) {
             float inv[2];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) inv[x] = __builtin_amdgcn_rcpf(fmaxf(sc[x][0], sc[x][1]));
+            for (int x = 0; x < 2; ++x) inv[x] = __builtin_amdgcn_rcpf(fmaxf(fmaxf(sc[x][0], sc[x][1]), kLeastScale));
 #pragma unroll
             for (int g = 0; g < 2; ++g) share[g][i] = pack_f16x2(sc[0][g] * inv[0], sc[1][g] * inv[1]);
           }

@@ -286,6 +286,22 @@ def test_the_same_again_and_on_two_streams():
         assert torch.equal(out, want[i % 2][0])
 
 
+@pytest.mark.parametrize("rows", [1, 20, 33, 300])
+@pytest.mark.parametrize("G", [128, 64])
+def test_rows_that_were_never_written_are_zeros(G, rows):
+    """Pages of a new pool hold scales of 0: keys and values of 0 for the softmax.  (Rows of the lists keep the bit that says they are
+    read elsewhere: without it they would count here as well.)"""
+    s = Sequences([150, 40], [rows, 1], 2, G, 32, Hq=4, salient=[3, 60]).fill_pages()
+    for page in (int(s.cache.table[0, 1]), int(s.cache.table[1, 0])):
+        s.cache.k_codes[page] = 0
+        s.cache.v_codes[page] = 0
+        s.cache.k_meta[page] &= 0x8000
+        s.cache.v_meta[page] &= 0x8000
+    for n_split in (1, 2):
+        out, lse = _run(s, n_split)
+        check_attention(s, out, lse, SM)
+
+
 def test_tables_and_caches_that_the_caller_made():
     """The two tensors that the caller may replace are looked at; a cache that describes itself is asked."""
     s = Sequences([70, 3], [2, 1], 2, 128, Hq=4).fill_pages()
