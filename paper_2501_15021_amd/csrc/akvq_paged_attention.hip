@@ -380,6 +380,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
   int b = blockIdx.x / c.Hkv, head = blockIdx.x % c.Hkv, tile = gridDim.y - 1 - blockIdx.y;  // the rows that see most first
   // Unequal sequences, where a CU gets few workgroups: which ones decides.  Where it holds one (many rows), the longest begin first; where it
   // holds two or three, the first on every CU go from long to short, the second from short to long.
+  ChunkSpan s;
   if (MANY ? c.B <= kWave : c.B <= kWave && gridDim.x > kCus && gridDim.y * gridDim.z == 1) {
     const int me = min(lane, c.B - 1);
     const ChunkSpan mine = chunk_span(c.seq_len[me], c.row_start[me], c.row_start[me + 1], c);
@@ -400,9 +401,11 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
     if (here == 0ull) return;  // whole workgroup
     b = __builtin_ctzll(here);
     tile = __builtin_amdgcn_readlane(begin + tiles, b) - 1 - at;
+    s = {__builtin_amdgcn_readlane(mine.len, b), __builtin_amdgcn_readlane(mine.first, b), __builtin_amdgcn_readlane(mine.rows, b)};
+  } else {
+    s = chunk_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
   }
   const int unit = b * c.Hkv + head;
-  const ChunkSpan s = chunk_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
   const int rows = s.rows * R;                                  // of this unit: token by token, the heads of the group
   const int wg_row = tile * kRows;                              // first row of the workgroup
   if (wg_row >= rows) return;                                   // whole workgroup
@@ -410,6 +413,27 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
   const bool idle = row0 >= rows;                               // (of a workgroup whose wavefronts have rows of their own)
   const int my_row = min(row0 + col, rows - 1), my_token = my_row / R;
   const float sm2 = a.sm_scale * kLog2e;
+
+  const uint16_t *q_at = a.q + (s.first + my_token) * a.q_stride + (head * R + my_row - my_token * R) * kD + 8 * g_lane;
+  // the query as it arrives: a chunk of eight channels for every k (read again by each kind of keys: kept, it would take 32 registers all along)
+  auto load_query = [&](u32x4 (&raw)[NC]) {
+#pragma unroll
+    for (int k = 0; k < NC; ++k) raw[k] = *reinterpret_cast<const u32x4 *>(q_at + kD / NC * k);
+  };
+  // Few rows: what needs nothing but the sequence is asked for in front of the search for its 16-bit rows: the query, and the pages' numbers where
+  // two loads hold them all (lane l: of pages window + l and window + 64 + l)
+  const int32_t *table = c.table + (size_t)b * c.max_pages;
+  auto ask_table = [&](int from) { return table[min(from + lane, c.max_pages - 1)]; };
+  const bool short_table = c.max_pages <= 2 * kWave;
+  [[maybe_unused]] int window = 0, pages = 0, next_pages = 0;
+  [[maybe_unused]] u32x4 early_query[NC];
+  if constexpr (!MANY) {
+    if (short_table) {
+      pages = ask_table(0);
+      next_pages = ask_table(kWave);
+    }
+    load_query(early_query);
+  }
 
   // ---- the keys of this workgroup: blocks of 32 code rows, of 32 overlay slots, of 32 chunk rows, dealt to the splits as one list
   const int32_t *sidx = c.sal_idx + (size_t)unit * c.S_cap;
@@ -445,16 +469,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
   // per column: the reference that weights are relative to, from which excess over it it is raised (before the first score: any), and
   // this lane's share of the sum
   float m = 0.0f, limit = 0.5f * kNoScore, l = 0.0f;
-  const uint16_t *q_at = a.q + (s.first + my_token) * a.q_stride + (head * R + my_row - my_token * R) * kD + 8 * g_lane;
-  // the query as it arrives: a chunk of eight channels for every k (read again by each kind of keys: kept, it would take 32 registers all along)
-  auto load_query = [&](u32x4 (&raw)[NC]) {
-#pragma unroll
-    for (int k = 0; k < NC; ++k) raw[k] = *reinterpret_cast<const u32x4 *>(q_at + kD / NC * k);
-  };
   // the rotated query, times sm_scale * log2(e): products with it are base-2 logits
-  auto rotated = [&](float (&x)[8 * NC]) {
-    u32x4 raw[NC];
-    load_query(raw);
+  auto rotated = [&](const u32x4 (&raw)[NC], float (&x)[8 * NC]) {
     float f = sm2;
     if (!a.q_rotated) {
       rotate_query_columns(raw, x, lane);
@@ -534,7 +550,6 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
     for (int g = 0; g < NG; ++g) acc_z[g] = 0.0f;
 
     const ExpandF4 ex4;
-    const int32_t *table = c.table + (size_t)b * c.max_pages;
     struct Where { size_t row; int limit; };  // first row of a block in the pools; rows from `limit` on (of the sequence) take no part
     auto find = [&](int blk, int page) {
       const bool there = page >= 0 && page < c.n_pages;
@@ -553,23 +568,22 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
     const int first = code_begin;
     // Few rows, bound by the stream: blocks in pairs, whose rows' meta words are decoded a row a lane.  Keys and values of the next pair are asked
     // for as soon as this one's are used up, meta words of the one after it in front of them, and the first ones in front of the query's
-    // preparation.  The pages' numbers come 64 at a time (lane l: of block window + l), another 64 ahead: one a block, by a scalar load,
-    // would be waited for with the next access to LDS.
+    // preparation.  The pages' numbers come 64 at a time, another 64 ahead: one a block, by a scalar load, would be waited for with the next
+    // access to LDS.
     const int few_last = min(max(code_end, first + 1), n_code) - 1;  // (a wavefront without code rows asks for some block that there is)
-    auto ask_pages = [&](int from, int last) { return table[min(min(from + lane, last) * 32, s.len - 1) >> c.page_shift]; };
-    int window = first, pages = 0, next_pages = 0;
+    auto page_of = [&](int blk) { return (blk * 32) >> c.page_shift; };
     struct Pair { Where at[2]; };
     auto locate = [&](int blk) {  // in ascending order
       Pair p;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const int at = min(blk + x, few_last);
-        if (at - window >= kWave) {
+        const int at = min(blk + x, few_last), page = page_of(at);
+        if (page - window >= kWave) {
           window += kWave;
           pages = next_pages;
-          next_pages = ask_pages(window + kWave, few_last);
+          next_pages = ask_table(window + kWave);
         }
-        p.at[x] = find(at, __builtin_amdgcn_readlane(pages, at - window));
+        p.at[x] = find(at, __builtin_amdgcn_readlane(pages, page - window));
         if (blk + x >= code_end) p.at[x].limit = 0;
       }
       return p;
@@ -584,9 +598,11 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
     auto row_there = [&](int blk, const Pair &p) { return (blk + (lane >> 5)) * 32 + (lane & 31) < (lane < 32 ? p.at[0].limit : p.at[1].limit); };
     Pair now = {}, next = {};
     if constexpr (!MANY) {
-      window = min(first, few_last);
-      pages = ask_pages(window, few_last);
-      next_pages = ask_pages(window + kWave, few_last);
+      if (!short_table) {
+        window = page_of(min(first, few_last));
+        pages = ask_table(window);
+        next_pages = ask_table(window + kWave);
+      }
       now = locate(first);
       ask_meta(now);
 #pragma unroll
@@ -605,7 +621,13 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
     };
     {
       float x[8 * NC], mx = 0.0f;
-      rotated(x);
+      if constexpr (MANY) {
+        u32x4 raw[NC];
+        load_query(raw);
+        rotated(raw, x);
+      } else {
+        rotated(early_query, x);
+      }
 #pragma unroll
       for (int e = 0; e < 8 * NC; ++e) mx = fmaxf(mx, fabsf(x[e]));
       mx = T::column_max(mx);
@@ -867,13 +889,14 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
           for (int j = 0; j < NB; ++j) o[j] = T::f16(bm.v[st][j][lane], w, o[j]);
         }
       };
-      int pages = ask_pages(first, n_code - 1);
-      ask(first, pages);
-      pages = ask_pages(first + kStageBlocks, n_code - 1);
+      auto ask_pages = [&](int from) { return table[page_of(min(from + lane, n_code - 1))]; };
+      int of_blocks = ask_pages(first);
+      ask(first, of_blocks);
+      of_blocks = ask_pages(first + kStageBlocks);
       for (int from = first, turn = 0; from < code_end; from += kStageBlocks, turn ^= 1) {
         expand(min(from + mine, n_code - 1), sh.blocks[turn][mine]);
-        ask(from + kStageBlocks, pages);
-        pages = ask_pages(from + 2 * kStageBlocks, n_code - 1);
+        ask(from + kStageBlocks, of_blocks);
+        of_blocks = ask_pages(from + 2 * kStageBlocks);
         lds_barrier();  // (the other set was last read in front of the barrier before)
         if (idle) continue;
         const int last = min(kStageBlocks, code_end - from);
@@ -1000,8 +1023,10 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
   // ================= 16-bit rows of the cache =================
   if (wide_begin < wide_end) {
     {
+      u32x4 raw[NC];
       float x[8 * NC];
-      rotated(x);
+      load_query(raw);
+      rotated(raw, x);
       split_query(x);
     }
     const uint16_t *ks = c.k_sal + (size_t)unit * c.S_cap * kD, *vs = c.v_sal + (size_t)unit * c.S_cap * kD;

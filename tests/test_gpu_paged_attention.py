@@ -58,6 +58,16 @@ def test_tiles_of_every_size(lens, rows, Hq, Hkv):
         check_attention(s, out, lse, SM, f"n_split {n_split}")
 
 
+@pytest.mark.parametrize("rows", [1, 20, 70])
+@pytest.mark.parametrize("length,page_rows", [(2040, 32), (4070, 32), (4200, 32), (9000, 32), (20000, 64), (11000, 1024)])
+def test_tables_of_every_length(length, page_rows, rows):
+    """Page numbers come 64 at a time: tables of up to 64 pages, of up to 128, and longer ones, begun anywhere."""
+    s = Sequences([length, 100], [rows, 1], 1, 128, page_rows, Hq=2, salient=SALIENT, seed=length).fill_pages()
+    for n_split in (1, 2, 9):
+        out, lse = _run(s, n_split)
+        check_attention(s, out, lse, SM, f"n_split {n_split}")
+
+
 def test_default_splits_of_the_callers_bound():
     """The library's choice is that of the max_rows it is given, also where fewer rows come: a workspace of that size serves them."""
     s = Sequences([3000, 40], [1, 0], 2, 128, Hq=4, salient=SALIENT, seed=2).fill_pages()
