@@ -28,7 +28,7 @@
 // matrix product of 8192 x 8192 x 8192: 1268); first chunks of 4096, which LDS reads bind as much, 0.28 ms, 780.
 //   Tiles of 16 and 32 read the cache with what their wavefronts have under way.  One row of 4 heads over 32768 rows of 128 units (G = 64):
 // 94-97 us, 3.6 TB/s, where vector instructions take 63 % of the time and matrix instructions 27; one row over 2048 to 4096 rows of 512 units 36 us, 3.2
-// TB/s, 13 of it before the first block and behind the last: two wavefronts a SIMD, 42 and 14 %.  One row over 640 of 32 units: 8.5 us and 2.8
+// TB/s, 13 of it before the first block and behind the last: two wavefronts a SIMD, 42 and 14 %.  One row over 640 of 32 units: 8.0 us and 2.8
 // for the merge, a chain of memory round trips.
 #include "akvq_device.h"
 #include "akvq_kernels.h"
