@@ -417,28 +417,14 @@ struct PagedAttentionArgs {
 };
 hipError_t launch_paged_attention(const PagedAttentionArgs &a, int G, hipStream_t stream);
 constexpr int kPagedManyRows = 256;  // of a workgroup that has many; its number is a grid dimension
-// How many rows (tokens x heads of a group) a workgroup takes of units (sequences x KV heads) with at most `tokens` tokens of R heads over
-// at most `len` cached rows: 16 or 32, which its four wavefronts share, or 256, 32 for each of eight.  Measured, us (G = 128 but where it
-// says 64, R = 1 but where it says more):
-//   17 to 32 rows, two tiles of 16 or one of 32: little to read, where a tile's beginning and end count, 8 units x 32768 cached rows 20.3
-//     and 25.7 (R = 4); much, where reading twice counts, 32 x 32768 40.0 and 39.5 (R = 4), 128 x 16384 (R = 7, G = 64) 91.5 and 68.7;
-//   tiles of 32 or of 256: one tile of 256 takes as long with three wavefronts of work as with one: 256 units of 96 rows 85 and 97, of 200
-//     188 and 151; 128 of 128 rows 95 and 112, of 256 185 and 172.  While the tiles of 32 leave no CU more than two workgroups they win
-//     for longer: 64 units of 256 rows 94 and 102, 4 of 585 tokens (R = 7) over 2048 cached rows 39 and 54, but over many keys, which eight
-//     wavefronts expand and stage together, only as long as there is nothing to split: 4 of 1024 (R = 4) over 32768 320 and 302, 4 of 4096 over 64
-//     71 and 59.
-inline int paged_tile_rows(long units, long tokens, long R, long len) {
-  const long rows = tokens * R;
-  if (rows <= 16 || (rows <= 32 && units * ((len + 31) / 32) < 1L << 15)) return 16;
-  return rows <= 128 || (units * ((rows + 31) / 32) <= 512 && len + 4 * tokens <= 16384) ? 32 : kPagedManyRows;
-}
-// How many splits of the keys.  A workgroup's beginning and end and the merge cost as much as some blocks of 32 keys, so the CUs are
-// filled once with few blocks a workgroup, and further (as many as run together on a CU) only with many.  Measured, us: one row over 16384
-// cached rows of 32 units, 256 workgroups 21.1, 512 18.1, 768 20.1; of 256 units, 256 106, 512 79, 768 72; 32 rows (R = 4) over 32768 of 32 units,
-// 256 40.4, 512 37.0; of 256 units over 4096, 256 38.5, 512 42.7, over 8192 70 and 64; one row over 640 of 32 units, 2 splits 10.8, 5
+// How many splits of the keys, for units (sequences x KV heads) with at most `tokens` tokens of R heads over at most `len` cached rows, in
+// tiles of `per` rows.  A workgroup's beginning and end and the merge cost as much as some blocks of 32 keys, so the CUs are filled once with
+// few blocks a workgroup, and further (as many as run together on a CU) only with many.  Measured, us: one row over 16384 cached rows of
+// 32 units, 256 workgroups 21.1, 512 18.1, 768 20.1; of 256 units, 256 106, 512 79, 768 72; 32 rows (R = 4) over 32768 of 32 units, in tiles of
+// 32, 256 40.4, 512 37.0; of 256 units over 4096, 256 38.5, 512 42.7, over 8192 70 and 64; one row over 640 of 32 units, 2 splits 10.8, 5
 // splits 9.5.
-inline int paged_splits(long units, long tokens, long R, long len) {
-  const long blocks = (len + 31) / 32, per = paged_tile_rows(units, tokens, R, len), tiles = (tokens * R + per - 1) / per;
+inline long paged_tile_splits(long per, long units, long tokens, long R, long len) {
+  const long blocks = (len + tokens + 31) / 32, tiles = (tokens * R + per - 1) / per;
   long want = 1;
   auto fill = [&](long workgroups, long least) {
     long n = workgroups / (units * tiles);
@@ -448,7 +434,33 @@ inline int paged_splits(long units, long tokens, long R, long len) {
   if (per == 16) { fill(256, 4); fill(512, 8); fill(768, 64); }
   else if (per == 32) { fill(256, 8); fill(512, want == 1 ? 128 : 32); }
   else fill(256, 8);
-  return (int)(want < 64 ? want : 64);
+  return want < 64 ? want : 64;
+}
+// What a call takes in tiles of 32 or 256 rows, in us, by rounds of workgroups (two on a CU, or one): a beginning and end, and for every block
+// of 32 keys what was measured on full CUs.  Within 15 % of the measurements below; it is there to compare the two.
+inline double paged_tile_cost(long per, long units, long tokens, long R, long len) {
+  const long rows = tokens * R, tiles = (rows + per - 1) / per, splits = paged_tile_splits(per, units, tokens, R, len);
+  const double cached = len / 32.0, own = tokens / 32.0, merge = splits > 1 ? 5.0 : 0.0;
+  double rounds = (double)(units * tiles * splits) / (per == 32 ? 512 : 256);
+  if (rounds < 1.0) rounds = 1.0;
+  if (per == 32) return rounds * (10.0 + (0.32 * cached + 0.5 * own) / splits) + merge;
+  return rounds * (18.0 + (0.44 + 0.1 * (rows / 32.0 / tiles)) * (cached + own) / splits) + merge;  // (per wavefront that has rows)
+}
+// How many rows (tokens x heads of a group) a workgroup takes: 16 or 32, which its four wavefronts share, or 256, 32 for each of eight that
+// look at the same keys.  Measured, us (G = 128 but where it says 64, R = 1 but where it says more):
+//   17 to 32 rows, two tiles of 16 or one of 32: little to read, where a tile's beginning and end count, 8 units x 32768 cached rows 20.3
+//     and 25.7 (R = 4); much, where reading twice counts, 32 x 32768 40.0 and 39.5 (R = 4), 128 x 16384 (R = 7, G = 64) 91.5 and 68.7;
+//   tiles of 32 or of 256, the better split of each: 256 units of 96 rows over 4096 85 and 97, of 200 188 and 151; 128 of 128 rows over 8192 95 and
+//     112, of 256 185 and 172; 64 of 256 94 and 102; 4 of 585 tokens (R = 7) over 2048 39 and 54; 4 of 1024 (R = 4) over 32768 320 and 302;
+//     4 of 4096 over 64 71 and 59, 8 of 2048 42 and 48.
+inline long paged_tile_rows(long units, long tokens, long R, long len) {
+  const long rows = tokens * R;
+  if (rows <= 16 || (rows <= 32 && units * ((len + 31) / 32) < 1L << 15)) return 16;
+  if (rows <= 64) return 32;
+  return paged_tile_cost(32, units, tokens, R, len) <= paged_tile_cost(kPagedManyRows, units, tokens, R, len) ? 32 : kPagedManyRows;
+}
+inline int paged_splits(long units, long tokens, long R, long len) {
+  return (int)paged_tile_splits(paged_tile_rows(units, tokens, R, len), units, tokens, R, len);
 }
 
 // status of a launch for the C ABI; keeps a failed launch's code for akvq_last_hip_error (akvq_api.hip)

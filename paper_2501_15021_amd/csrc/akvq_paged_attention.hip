@@ -1361,7 +1361,7 @@ void launch_variant(const PagedAttentionArgs &a, int rows, hipStream_t stream) {
   auto grid = [&](int per) { return dim3(units, (rows + per - 1) / per, a.n_split); };
   constexpr int kFew = 64 * kFewWaves, kMany = 64 * kManyWaves;
   static_assert(kPagedManyRows == 32 * kManyWaves);
-  const int per = paged_tile_rows(units, a.c.max_rows, a.Hq / a.c.Hkv, a.c.max_len);
+  const long per = paged_tile_rows(units, a.c.max_rows, a.Hq / a.c.Hkv, a.c.max_len);
   if (per == 16) paged_attention_kernel<G, 16, false><<<grid(16), kFew, 0, stream>>>(a);
   else if (per == 32) paged_attention_kernel<G, 32, false><<<grid(32), kFew, 0, stream>>>(a);
   else paged_attention_kernel<G, 32, true><<<grid(kPagedManyRows), kMany, 0, stream>>>(a);
