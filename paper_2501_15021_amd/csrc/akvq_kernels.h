@@ -457,6 +457,7 @@ inline long paged_tile_rows(long units, long tokens, long R, long len) {
   const long rows = tokens * R;
   if (rows <= 16 || (rows <= 32 && units * ((len + 31) / 32) < 1L << 15)) return 16;
   if (rows <= 64) return 32;
+  if (rows > 65535L * 32) return kPagedManyRows;  // (tiles are a grid dimension)
   return paged_tile_cost(32, units, tokens, R, len) <= paged_tile_cost(kPagedManyRows, units, tokens, R, len) ? 32 : kPagedManyRows;
 }
 inline int paged_splits(long units, long tokens, long R, long len) {
