@@ -319,7 +319,8 @@ int akvq_rope_axes_table(const akvq_axes *axes, const int32_t *pos, int64_t pos_
  *   table: device, [B][max_pages] int32: row t of sequence b is row t % page_rows of page table[b][t / page_rows].  An entry outside
  *     [0, n_pages) names no page: rows meant for it are dropped, and its rows take no part in attention.  No page may be named twice
  *     where rows are written.  seq_len: device, [B] int32: cached rows.  max_len: an upper bound of them that the host knows (what
- *     lies behind it takes no part); it sizes launches and workspaces, so one bound for many steps keeps a captured call valid.
+ *     lies behind it takes no part in attention); it sizes that call's launches and workspaces, so one bound for many steps keeps a
+ *     captured call valid.  Where rows are written goes by seq_len alone.
  *   The 16-bit rows are the sequences' own, as in akvq_cache: k_sal, v_sal, sal_idx [B][Hkv][S_cap] (positions of the sequence,
  *     ascending), sal_cnt [B][Hkv].
  *   max_pages * page_rows must stay below 2^30.  table, seq_len and row_start need 4-byte alignment only.
@@ -346,7 +347,8 @@ int akvq_paged_bytes(const akvq_paged *shape, size_t out_bytes[8]);
 /*
  * akvq_paged_append -- the write path into pages: the chunk's rows of sequence b become its cache rows seq_len[b],
  *   seq_len[b] + 1, ..., with the codes, meta words, salient bits and overlay rows that akvq_quantize_append writes for them, bit for
- *   bit.  k, v: post-RoPE, un-rotated.  Rows behind the table's last page are dropped.  The salient lists must be final for these rows.
+ *   bit.  k, v: post-RoPE, un-rotated.  Rows behind the table's last page are dropped, and all rows of a sequence whose seq_len is negative.
+ *   The salient lists must be final for these rows.
  *   flags: AKVQ_K_PREROTATED, AKVQ_V_PREROTATED.  Does not modify seq_len.  n_rows = 0 does nothing.
  */
 int akvq_paged_append(const akvq_paged *c, const akvq_chunk *rows, const void *k, int64_t k_stride, const void *v,

@@ -457,7 +457,8 @@ class PagedCache:
 
     The caller owns the page table: it writes page numbers into table [B, max_pages] (-1: no page) and advances seq_len [B], both int32
     on the device, so that calls can be captured and replayed while they change.  max_len is what the host knows of the longest
-    sequence (by default all that the table can name); it only sizes launches.  select_salient takes a PagedCache, too."""
+    sequence (by default all that the table can name): it sizes attention's launches, and rows behind it take no part there;
+    paged_append stores rows at seq_len whatever it is.  select_salient takes a PagedCache, too."""
 
     def __init__(self, B: int, Hkv: int, G: int, n_pages: int, max_pages: int, page_rows: int = 64, S_cap: int = 64, device="cuda",
                  fill: Optional[int] = None):

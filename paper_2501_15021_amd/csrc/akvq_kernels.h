@@ -395,6 +395,14 @@ __host__ __device__ inline ChunkSpan chunk_span(int len, int first, int end, con
   s.rows = end - s.first < a.max_rows ? end - s.first : a.max_rows;
   return s;
 }
+// ... as the write path takes it: rows go where the device's length says, whatever bound of it the host has, and a length that names no row of
+// the table leaves no place for any.
+__host__ __device__ inline ChunkSpan append_span(int len, int first, int end, const PagedArgs &a) {
+  ChunkSpan s = chunk_span(0, first, end, a);
+  s.len = len;
+  if (len < 0 || len >= a.row_cap) s.rows = 0;
+  return s;
+}
 struct PagedAppendArgs {
   PagedArgs c;
   const uint16_t *k, *v;

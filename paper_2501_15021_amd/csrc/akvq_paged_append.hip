@@ -43,10 +43,11 @@ __device__ __forceinline__ void paged_append_body(const PagedAppendArgs &a, int 
   const PagedArgs &c = a.c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int b = blockIdx.y / c.Hkv, head = blockIdx.y % c.Hkv, r = lane >> 2, j = lane & 3;
-  const ChunkSpan s = chunk_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
+  const ChunkSpan s = append_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
+  if (s.rows == 0) return;  // whole wavefront leaves (here and below); no workgroup barrier below
   const int t_end = min(s.len + s.rows, c.row_cap);
   const int blk = s.len / kTokBlock + blockIdx.x * 4 + wave, t0 = blk * kTokBlock;
-  if (s.rows == 0 || t0 >= t_end) return;  // whole wavefront leaves; no workgroup barrier below
+  if (t0 >= t_end) return;
   const int page = c.table[(size_t)b * c.max_pages + (t0 >> c.page_shift)];
   if (page < 0 || page >= c.n_pages) return;
   const int t_page = t0 & ((1 << c.page_shift) - 1);  // the block's first row in its page
@@ -231,8 +232,8 @@ __global__ __launch_bounds__(64) void paged_append_row_kernel(PagedAppendArgs a)
   __shared__ __attribute__((aligned(16))) uint16_t row_lds[kD];
   const PagedArgs &c = a.c;
   const int unit = blockIdx.x, b = unit / c.Hkv, head = unit % c.Hkv;
-  const ChunkSpan s = chunk_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
-  if (s.rows == 0 || s.len >= c.row_cap) return;
+  const ChunkSpan s = append_span(c.seq_len[b], c.row_start[b], c.row_start[b + 1], c);
+  if (s.rows == 0) return;
   const int page = c.table[(size_t)b * c.max_pages + (s.len >> c.page_shift)];
   if (page < 0 || page >= c.n_pages) return;
   const int t0 = s.len & ~(kTokBlock - 1);
