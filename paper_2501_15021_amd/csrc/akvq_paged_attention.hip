@@ -313,8 +313,16 @@ struct CodeBlock {
   __attribute__((aligned(16))) float k_scale[NG][32];
   __attribute__((aligned(16))) float v_rcp[32];                       // 1 / V scale, the larger one where there are two (no part: 0)
   __attribute__((aligned(16))) u32x4 k[2][kWave];                     // [product][lane] codes as 4-bit floats
-  __attribute__((aligned(16))) u32x4 v[2][4][kWave];                  // [step][channel block][lane] (code - zero-point) * share of the larger scale, binary16
+  __attribute__((aligned(16))) u32x4 v[2][4][kWave];                  // [step][channel block][lane] (code - low part of the zero-point) * share of the larger scale, binary16
+  // where some zero-point has one: minus its multiple of 1024, in the weights' order; of two groups times the share, in two binary16 terms
+  __attribute__((aligned(16))) uint16_t v_far[NG][NG][32];
 };
+// A value's zero-point: a low part, -512 to 511, and a multiple of 1024.  The first of two rows' as binary16 numbers -1536 - low: those from -1024 to
+// -2047 hold ten bits as they are.
+__device__ __forceinline__ uint32_t less_zero_low(uint32_t meta0, uint32_t meta1) {
+  return (__builtin_amdgcn_perm(meta1, meta0, 0x07060302u) & 0x03FF03FFu) ^ 0xE600E600u;
+}
+__device__ __forceinline__ int zero_high(uint32_t meta) { return (((int)meta >> 16) + 512) & ~1023; }
 
 __device__ __forceinline__ void lds_barrier() {  // leaves loads from memory in flight
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -332,7 +340,10 @@ struct PagedShared;
 template <int G, int W>
 struct PagedShared<G, W, true> {
   union {  // code rows come first, then 16-bit rows
-    CodeBlock<kD / G> blocks[2][kStageBlocks];  // being worked on, and the next
+    struct {
+      CodeBlock<kD / G> blocks[2][kStageBlocks];  // being worked on, and the next
+      __attribute__((aligned(4))) uint8_t far[2][kStageBlocks];  // whether v_far is written
+    };
     struct { __attribute__((aligned(16))) uint16_t k[2][kStage * kD], v[2][kStage * kD]; };
   };
 };
@@ -810,11 +821,11 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
 #pragma unroll
           for (int y = 0; y < NG; ++y) v_meta[x][y] = *reinterpret_cast<const u32x4 *>(meta + 16 * NG * x + 4 * y);
         v = *reinterpret_cast<const u32x2 *>(c.v_codes + at.row * 8 + (16 * (2 * part + h) + n) * 4 + 2 * p);
-        if (part == 0) words = load_meta<NG>((lane < 32 ? c.k_meta : c.v_meta) + (at.row + (lane & 31)) * NG);
-        else k = load_codes(c.k_codes, at);
+        words = load_meta<NG>((part == 0 && lane < 32 ? c.k_meta : c.v_meta) + (at.row + (lane & 31)) * NG);
+        if (part == 1) k = load_codes(c.k_codes, at);
         limit = at.limit;
       };
-      auto expand = [&](int blk, CodeBlock<NG> &to) {
+      auto expand = [&](int blk, CodeBlock<NG> &to, uint8_t &far_zero) {
         if (part == 0) {
           const int r = lane & 31;  // lanes 0-31: keys, lanes 32-63: values
           const RowMeta<NG> row(words, blk * 32 + r < limit, lane >= 32);
@@ -825,23 +836,40 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
           const u32x2 k0 = ex4(k[0]), k1 = ex4(k[1]), k2 = ex4(k[2]), k3 = ex4(k[3]);
           to.k[0][lane] = (u32x4){k0[0], k0[1], k2[0], k2[1]};
           to.k[1][lane] = (u32x4){k1[0], k1[1], k3[0], k3[1]};
+          int high[NG], any = 0;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) any |= high[g] = zero_high(words.w[g]);
+          const bool far = __ballot(any != 0) != 0ull;
+          if (lane == 0) far_zero = far;
+          if (__builtin_expect(far, 0)) {  // (two lanes a row)
+            const int r = lane & 31;
+            const RowMeta<NG> row(words, blk * 32 + r < limit, true);
+            const int at = 2 * (4 * ((r & 15) >> 2) + (r & 3)) + (r >> 4);  // the weights' order: pairs (r, r + 16)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              const float z = -(float)high[g] * (NG == 2 ? row.scale[g] * row.rcp : 1.0f);
+              const uint32_t a = float_to_half_bits_rne(z);
+              to.v_far[0][g][at] = (uint16_t)a;
+              if constexpr (NG == 2) to.v_far[1][g][at] = (uint16_t)float_to_half_bits_rne(z - half_bits_to_float(a));
+            }
+          }
         }
-        // values: 1024 + code in place, less 1024 + zero-point: exact up to zero-points of 1024, else to 2^-11 of them; where a row has two
-        // scales, times its share of the larger one, rounded (2^-11 again): one set of weights serves both groups
+        // values: 1536 + code in place, less 1536 + the low part of the zero-point: exact (the rest of a far one is summed apart); where a row has
+        // two scales, times its share of the larger one, rounded (2^-11): one set of weights serves both groups
         u32x4 less[NG], share[NG];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float z[2][NG], sc[2][NG];
+          [[maybe_unused]] float sc[2][NG];
 #pragma unroll
-          for (int x = 0; x < 2; ++x)
+          for (int g = 0; g < NG; ++g) {
+            uint32_t w[2];
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-              const uint32_t w = v_meta[x][NG == 2 ? i / 2 : 0][NG == 2 ? 2 * (i & 1) + g : i];
-              z[x][g] = (float)((int)w >> 16);
-              sc[x][g] = half_bits_to_float(w & 0x7FFFu);
+            for (int x = 0; x < 2; ++x) {
+              w[x] = v_meta[x][NG == 2 ? i / 2 : 0][NG == 2 ? 2 * (i & 1) + g : i];
+              sc[x][g] = half_bits_to_float(w[x] & 0x7FFFu);
             }
-#pragma unroll
-          for (int g = 0; g < NG; ++g) less[g][i] = pack_f16x2(-1024.0f - z[0][g], -1024.0f - z[1][g]);
+            less[g][i] = less_zero_low(w[0], w[1]);
+          }
           if constexpr (NG == 2) {
             float inv[2];
 #pragma unroll
@@ -864,7 +892,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
             u32x4 o4;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint32_t code = ((v[wd] >> (8 * x + 2 * i)) & 0x00030003u) | 0x64006400u, zi = less[g][i];
+              const uint32_t code = ((v[wd] >> (8 * x + 2 * i)) & 0x00030003u) | 0x66006600u, zi = less[g][i];
               f16x2 val = __builtin_bit_cast(f16x2, code) + __builtin_bit_cast(f16x2, zi);
               if constexpr (NG == 2) {
                 const uint32_t si = share[g][i];
@@ -878,15 +906,27 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       auto block_scores = [&](const CodeBlock<NG> &bm, float (&y)[NY]) {
         scores(bm, y, [&](int pr, int) { return bm.k[pr][lane]; });
       };
-      auto block_values = [&](const CodeBlock<NG> &bm, float (&y)[NY]) {
+      auto block_values = [&](const CodeBlock<NG> &bm, bool far, float (&y)[NY]) {
         weights(bm, y);
+        u32x4 w[NS];
 #pragma unroll
         for (int st = 0; st < NS; ++st) {
-          u32x4 w;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = pack_f16x2(y[4 * st + i], y[4 * st + NY / 2 + i]);
+          for (int i = 0; i < 4; ++i) w[st][i] = pack_f16x2(y[4 * st + i], y[4 * st + NY / 2 + i]);
 #pragma unroll
-          for (int j = 0; j < NB; ++j) o[j] = T::f16(bm.v[st][j][lane], w, o[j]);
+          for (int j = 0; j < NB; ++j) o[j] = T::f16(bm.v[st][j][lane], w[st], o[j]);
+        }
+        if (__builtin_expect(far, 0)) {  // rows far from zero: the same for all of a group's channels
+#pragma unroll
+          for (int st = 0; st < NS; ++st)
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+              for (int x = 0; x < NG; ++x) {
+                const u32x4 z = *reinterpret_cast<const u32x4 *>(&bm.v_far[x][g][8 * (2 * st + g_lane)]);
+#pragma unroll
+                for (int j = g * NB / NG; j < (g + 1) * NB / NG; ++j) o[j] = T::f16(z, w[st], o[j]);
+              }
         }
       };
       auto ask_pages = [&](int from) { return table[page_of(min(from + lane, n_code - 1))]; };
@@ -894,18 +934,19 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       ask(first, of_blocks);
       of_blocks = ask_pages(first + kStageBlocks);
       for (int from = first, turn = 0; from < code_end; from += kStageBlocks, turn ^= 1) {
-        expand(min(from + mine, n_code - 1), sh.blocks[turn][mine]);
+        expand(min(from + mine, n_code - 1), sh.blocks[turn][mine], sh.far[turn][mine]);
         ask(from + kStageBlocks, of_blocks);
         of_blocks = ask_pages(from + 2 * kStageBlocks);
         lds_barrier();  // (the other set was last read in front of the barrier before)
         if (idle) continue;
         const int last = min(kStageBlocks, code_end - from);
+        const uint32_t far = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t *>(&sh.far[turn][0]));  // (a byte a block)
         for (int x = 0; x < last; ++x) {
           const CodeBlock<NG> &bm = sh.blocks[turn][x];
           float y[NY];
           block_scores(bm, y);
           raise_codes(y);
-          block_values(bm, y);
+          block_values(bm, ((far >> (8 * x)) & 1u) != 0u, y);
         }
       }
       lds_barrier();  // the stages of 16-bit rows lie where the blocks were
