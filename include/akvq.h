@@ -361,7 +361,8 @@ int akvq_paged_append(const akvq_paged *c, const akvq_chunk *rows, const void *k
  *   stored them behind seq_len.  One row a sequence is the decode step of a batch of unequal lengths; nothing cached is a first chunk.
  *   q, k, v: post-RoPE, un-rotated.  out: [n_rows][Hq][128] binary16, rows out_stride elements apart.  lse_out: optional, [n_rows][Hq]
  *   fp32.  Hq / Hkv at most 8, max_rows * Hq / Hkv below 2^24 - 256.  fp32 scores, sums and accumulators; the cached rows' queries as
- *   integers of 20 bits (16 against 16-bit rows), weights of 11 bits (16 for the 16-bit rows).
+ *   integers of 20 bits (16 against 16-bit rows), weights of 11 bits (16 for the 16-bit rows), cached values as they are (with G = 64 and
+ *   hundreds of rows a sequence rounded to 11 bits once).
  *   Rows listed as salient are read from the overlay whatever their page.  NaN or infinity in a sequence's own rows gives
  *   unspecified values for that sequence and KV head, never for others.
  *   flags: AKVQ_Q_PREROTATED (q and k arrive rotated), AKVQ_OUT_ROTATED (the chunk's v rows arrive rotated, out is left rotated).

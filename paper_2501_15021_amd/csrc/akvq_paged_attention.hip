@@ -311,12 +311,15 @@ struct CodeBlock {
   __attribute__((aligned(16))) uint16_t start[32][2][8];              // as in BlockMeta
   __attribute__((aligned(16))) uint16_t start2[NG == 2 ? 32 : 1][8];
   __attribute__((aligned(16))) float k_scale[NG][32];
-  __attribute__((aligned(16))) float v_rcp[32];                       // 1 / V scale, the larger one where there are two (no part: 0)
+  __attribute__((aligned(16))) float v_rcp[32];                       // 1 / V scale, where there are two 1 / the larger one's power of two (no part: 0)
   __attribute__((aligned(16))) u32x4 k[2][kWave];                     // [product][lane] codes as 4-bit floats
-  __attribute__((aligned(16))) u32x4 v[2][4][kWave];                  // [step][channel block][lane] (code - low part of the zero-point) * share of the larger scale, binary16
+  __attribute__((aligned(16))) u32x4 v[2][4][kWave];                  // [step][channel block][lane] (code - low part of the zero-point) * share, binary16
   // where some zero-point has one: minus its multiple of 1024, in the weights' order; of two groups times the share, in two binary16 terms
   __attribute__((aligned(16))) uint16_t v_far[NG][NG][32];
 };
+// The power of two at or below a positive number: its logarithm and reciprocal (of 0: -127 and 2^127).
+__device__ __forceinline__ float power_log(float x) { return (float)((int)(__float_as_uint(x) >> 23) - 127); }
+__device__ __forceinline__ float power_rcp(float x) { return __uint_as_float(0x7F000000u - (__float_as_uint(x) & 0x7F800000u)); }
 // A value's zero-point: a low part, -512 to 511, and a multiple of 1024.  The first of two rows' as binary16 numbers -1536 - low: those from -1024 to
 // -2047 hold ten bits as they are.
 __device__ __forceinline__ uint32_t less_zero_low(uint32_t meta0, uint32_t meta1) {
@@ -829,9 +832,9 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
         if (part == 0) {
           const int r = lane & 31;  // lanes 0-31: keys, lanes 32-63: values
           const RowMeta<NG> row(words, blk * 32 + r < limit, lane >= 32);
-          const float v_log = halves(log2_bare(row.top)).hi;
+          const float v_log = halves(NG == 2 ? power_log(row.top) : log2_bare(row.top)).hi;
           if (lane < 32) decode_key(row, v_log, to, r);
-          else to.v_rcp[r] = row.rcp;
+          else to.v_rcp[r] = NG == 2 && row.part ? power_rcp(row.top) : row.rcp;
         } else {
           const u32x2 k0 = ex4(k[0]), k1 = ex4(k[1]), k2 = ex4(k[2]), k3 = ex4(k[3]);
           to.k[0][lane] = (u32x4){k0[0], k0[1], k2[0], k2[1]};
@@ -847,7 +850,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
             const int at = 2 * (4 * ((r & 15) >> 2) + (r & 3)) + (r >> 4);  // the weights' order: pairs (r, r + 16)
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-              const float z = -(float)high[g] * (NG == 2 ? row.scale[g] * row.rcp : 1.0f);
+              const float z = -(float)high[g] * (NG == 2 ? row.scale[g] * power_rcp(row.top) : 1.0f);
               const uint32_t a = float_to_half_bits_rne(z);
               to.v_far[0][g][at] = (uint16_t)a;
               if constexpr (NG == 2) to.v_far[1][g][at] = (uint16_t)float_to_half_bits_rne(z - half_bits_to_float(a));
@@ -855,7 +858,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
           }
         }
         // values: 1536 + code in place, less 1536 + the low part of the zero-point: exact (the rest of a far one is summed apart); where a row has
-        // two scales, times its share of the larger one, rounded (2^-11): one set of weights serves both groups
+        // two scales, times the group's over the larger one's power of two (its own bits, where it is above 2^-14), rounded once, 2^-11: one set of
+        // weights serves both groups
         u32x4 less[NG], share[NG];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -873,7 +877,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
           if constexpr (NG == 2) {
             float inv[2];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) inv[x] = __builtin_amdgcn_rcpf(fmaxf(fmaxf(sc[x][0], sc[x][1]), kLeastScale));
+            for (int x = 0; x < 2; ++x) inv[x] = power_rcp(fmaxf(sc[x][0], sc[x][1]));
 #pragma unroll
             for (int g = 0; g < 2; ++g) share[g][i] = pack_f16x2(sc[0][g] * inv[0], sc[1][g] * inv[1]);
           }

@@ -1,4 +1,4 @@
-"""Values of tiles of 256 rows (akvq_paged_attention): zero-points of any size, seen where every weight is the same, so that the
+"""Values of tiles of 256 rows (akvq_paged_attention): zero-points of any size and groups of different scales, seen where every weight is the same, so that the
 kernel's own sums are exact; and rows far from zero against the formula."""
 import pytest
 import torch
@@ -59,3 +59,9 @@ def _equal_weights(G, zeros, scales):
                                    [4095, -4096, 10000, -20001, 12345], [32767, -32768, 1025, -32767, 31743]])
 def test_zero_points_are_exact(zeros, G):
     _equal_weights(G, zeros, (2.0 ** -6, 2.0 ** -7))
+
+
+@pytest.mark.parametrize("scales", [(1.5, 1.0), (1.0, 1.75), (1.25, 0.75), (1.75, 0.0009765625), (0.625, 1.5)])
+def test_groups_of_different_scales_are_exact(scales):
+    """Values whose product with a scale of a few bits fits binary16."""
+    _equal_weights(64, [1, -5, 200, -190, 7], tuple(x * 2.0 ** -6 for x in scales))
