@@ -293,7 +293,7 @@ int akvq_decode_step(const akvq_cache *c, const uint32_t *fine_mask, const akvq_
  * akvq_rope_axes -- rotary positions on several axes (time, height and width of images and video): channel pair (i, i + 64) of
  *   a row is turned by the angle pos[axis[i]][row] * inv_freq[i], in the pairing of akvq_rope.  A pair with inv_freq 0 stays as
  *   it is.  pos: device, int32, any alignment of 4 bytes, n_axes rows pos_stride elements apart, one entry for every chunk row.
- *   The angle is formed in 64 bits and its whole turns are dropped there (an error of 1e-7 at the largest position), sine and
+ *   The angle is formed in twice 64 bits and its whole turns are dropped there (an error of 1e-7 radians for angles below 2^50), sine and
  *   cosine are 32-bit, the result is rounded to binary16 once.  (The fused embedding of akvq_rope reads a binary16 table instead:
  *   akvq_rope_axes_table writes one.)  flags: AKVQ_ROPE_INVERSE or 0.
  *   q_out / k_out may be q / k themselves with the same stride, else they may not overlap them.  Hkv = 0 (Hq = 0): no k (q).

@@ -1,7 +1,7 @@
 // Rotary positions with several axes: pair i of a row (channels i, i + 64) is turned by pos[axis(i)][row] * inv_freq(i).
 //
 // Memory bound: every element is read and written once for three operations.  One wavefront takes a row: lane i forms the angle of
-// pair i once for all heads (a 64-bit product, whose whole turns are dropped before 32 bits hold it: a 32-bit angle would be off by
+// pair i once for all heads (a 64-bit product and its rest, whose whole turns are dropped before 32 bits hold it: a 32-bit angle would be off by
 // 2^-24 of itself, 6e-3 at position 100000) and leaves its sine and cosine in LDS, from where lane (h, o) takes those of pairs
 // 8o .. 8o + 7 for every eighth head: two 128-bit loads and stores a head, 128 contiguous bytes for eight lanes.
 //   Measured: 8 x 8191 rows of 32 heads 131 us, 5.4 TB/s (a large copy: 5.47); sixteen rows of 64 heads 2.3 us, a launch and one round
@@ -17,8 +17,10 @@ constexpr int kAxesWaves = 4;
 
 // cosine and sine of a row's pair
 __device__ __forceinline__ void pair_turn(const AxesArgs &a, int pair, int row, float &c, float &s) {
-  const double t = (double)a.pos[a.axis[pair] * a.pos_stride + row] * a.turns[pair];
-  sincospif(2.0f * (float)(t - rint(t)), &s, &c);
+  const double p = a.pos[a.axis[pair] * a.pos_stride + row], f = a.turns[pair], t = p * f;
+  // what the rounded product and frequency leave: up to 5e-7 of an angle of 2^31, in place of 1e-7 for all
+  const double rest = __builtin_fma(p, f, -t) + p * (double)a.turns_rest[pair];
+  sincospif(2.0f * (float)((t - rint(t)) + rest), &s, &c);
 }
 
 __global__ __launch_bounds__(64 * kAxesWaves) void rope_axes_kernel(AxesArgs a) {

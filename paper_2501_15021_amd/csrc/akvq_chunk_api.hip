@@ -13,6 +13,9 @@ constexpr int kMaxChunkRows = 1 << 25;
 
 inline bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+// 1 / 2 pi as its first 29 bits, whose product with a 32-bit float is exact, and the rest
+constexpr double kTurns = 0x1.45f306dp-3, kTurnsRest = 0x1.9391054a7f09dp-32;
+
 // packed rows of `heads` heads, `stride` elements apart
 int check_rows(const void *rows, int64_t stride, int heads) {
   if (!rows || !aligned(rows, 16)) return AKVQ_ERR_INVALID_ARG;
@@ -27,7 +30,9 @@ int axes_args(const akvq_axes *axes, const int32_t *pos, int64_t pos_stride, int
   for (int i = 0; i < 64; ++i) {
     if (axes->axis[i] >= axes->n_axes) return AKVQ_ERR_INVALID_ARG;
     if (!__builtin_isfinite(axes->inv_freq[i])) return AKVQ_ERR_INVALID_ARG;
-    a.turns[i] = (double)axes->inv_freq[i] / 6.283185307179586476925;
+    const double whole = axes->inv_freq[i] * kTurns, rest = axes->inv_freq[i] * kTurnsRest;
+    a.turns[i] = whole + rest;
+    a.turns_rest[i] = (float)(rest - (a.turns[i] - whole));
     a.axis[i] = axes->axis[i];
   }
   if (n_rows > 0 && (!pos || !aligned(pos, 4))) return AKVQ_ERR_INVALID_ARG;
