@@ -436,7 +436,8 @@ class RopeAxes:
 def rope_axes(axes: RopeAxes, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None,
               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False):
     """akvq_rope_axes: rotary positions of a chunk's rows, q [n, Hq, 128] and k [n, Hkv, 128] (either may be None), into q_out and k_out
-    (new tensors where None; q and k themselves turn in place).  inverse: turns back, which is also the gradient.  Returns (q_out, k_out)."""
+    (new tensors where None; q and k themselves turn in place).  inverse: turns back, which is also the gradient; the call records none
+    itself and refuses rows that ask for one (a torch.autograd.Function calls it both ways).  Returns (q_out, k_out)."""
     st, outs = (_native or native()).rope_axes(axes._struct, pos, q, k, q_out, k_out, inverse)
     if st:
         _check(st, "akvq_rope_axes")

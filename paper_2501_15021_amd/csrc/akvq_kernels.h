@@ -360,7 +360,7 @@ hipError_t launch_stream_read(const void *src, size_t bytes, uint32_t *sink, int
 // ---- rotary positions with several axes (akvq_axes.hip) ----
 struct AxesArgs {
   double turns[64];  // per position, of channel pair i: inv_freq[i] / 2 pi ...
-  float turns_rest[64];  // ... and what its rounding left (in 64 bits the arguments would pass 1 KB, and a call that is waited for take 26 us in place of 18)
+  float turns_rest[64];  // ... and what its rounding left (in 64 bits the arguments would pass 1 KB, and a call that is waited for takes 26 us in place of 18)
   uint8_t axis[64];
   const int32_t *pos;
   long long pos_stride;

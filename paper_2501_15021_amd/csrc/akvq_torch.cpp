@@ -11,6 +11,7 @@
 #include <cstring>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -303,6 +304,10 @@ int64_t packed(const at::Tensor &t, const char *what, int64_t rows, int64_t head
   need(t.stride(2) == 1 && (t.size(1) == 1 || t.stride(1) == kHeadDim), what, ": the heads of a row have to lie next to each other");
   return t.size(0) > 1 ? t.stride(0) : t.size(1) * kHeadDim;
 }
+// No call here records a gradient.
+void no_gradient(const at::Tensor &t, const char *what) {
+  need(!t.requires_grad() || !c10::GradMode::is_enabled(), what, " asks for a gradient, which this call does not record (the inverse turns it back)");
+}
 at::Tensor fresh(at::IntArrayRef shape, const at::Tensor &like) { return at::empty(shape, like.options().dtype(at::kHalf).requires_grad(false)); }
 
 akvq_axes axes_of(PyObject *o) {  // the description that RopeAxes holds
@@ -353,6 +358,8 @@ PyObject *rope_axes(PyObject *, PyObject *const *a, Py_ssize_t n) {
       x[i].stride = packed(t, what[i], rows, -1);
       outs[i] = a[4 + i] == Py_None ? fresh(t.sizes(), t) : tensor(a[4 + i]);
       x[i].out_stride = packed(outs[i], what_out[i], rows, t.size(1));
+      no_gradient(t, what[i]);
+      no_gradient(outs[i], what_out[i]);
       x[i].in = t.data_ptr();
       x[i].out = outs[i].data_ptr();
       x[i].heads = count(t.size(1), "heads");
