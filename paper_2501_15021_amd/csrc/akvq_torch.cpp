@@ -304,6 +304,10 @@ int64_t packed(const at::Tensor &t, const char *what, int64_t rows, int64_t head
   need(t.stride(2) == 1 && (t.size(1) == 1 || t.stride(1) == kHeadDim), what, ": the heads of a row have to lie next to each other");
   return t.size(0) > 1 ? t.stride(0) : t.size(1) * kHeadDim;
 }
+// The call writes into the caller's tensor, which autograd has to know of (inference tensors have no count of their changes).
+void written(const at::Tensor &t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // No call here records a gradient.
 void no_gradient(const at::Tensor &t, const char *what) {
   need(!t.requires_grad() || !c10::GradMode::is_enabled(), what, " asks for a gradient, which this call does not record (the inverse turns it back)");
@@ -384,6 +388,8 @@ PyObject *rope_axes(PyObject *, PyObject *const *a, Py_ssize_t n) {
                               x[1].in, x[1].stride, x[1].heads, x[0].out, x[0].out_stride, x[1].out, x[1].out_stride,
                               inverse ? AKVQ_ROPE_INVERSE : 0, stream);
       Py_END_ALLOW_THREADS
+      for (int i = 0; i < 2; ++i)
+        if (a[4 + i] != Py_None) written(outs[i]);
     }
     Held out[2];
     for (int i = 0; i < 2; ++i) {
@@ -544,6 +550,8 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
       status = akvq_paged_attention(&pages.c, &chunk, q_at, qs, Hq, k_at, ks, v_at, vs, sm_scale, out_at, os,
                                     static_cast<float *>(lse_at), n_split, ws_at, bytes, flags, stream);
       Py_END_ALLOW_THREADS
+      if (a[9] != Py_None) written(out);
+      if (lse.defined()) written(lse);
     }
     Held o(a[9] == Py_None ? THPVariable_Wrap(out) : Py_NewRef(a[9]));
     if (!o.p) return nullptr;
