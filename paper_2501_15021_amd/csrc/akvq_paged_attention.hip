@@ -17,8 +17,8 @@
 //   V codes are masked in place, which leaves binary16 subnormals code * 4^ii * 2^-24 (ii: the row's place in its word): one
 // instruction per two codes.  The V scale and 4^-ii ride in the exponent of the weight, the denominator takes the weight back by
 // 4^ii / scale, and zero-points are summed with the rounded weights.
-//   Weights are binary16 (half a step is 2^-12 of a weight), relative to a reference that keeps the largest between 2^7 and 2^15: a
-// weight below 2^-21 of its row's largest loses bits, one below 2^-31 all of them.  Scores, references, sums and accumulators are 32-bit.
+//   Weights are binary16 (half a step is 2^-12 to 2^-11 of a weight; up to eight rows in a tile have two that round apart), relative to a reference
+// that keeps the largest between 2^7 and 2^15: a weight below 2^-21 of its row's largest loses bits, one below 2^-31 all of them.  Scores, references, sums and accumulators are 32-bit.
 //   Rows of a unit (a sequence's tokens times the heads of a KV head) come in tiles of 16 or 32 whose four wavefronts share the rows and deal
 // the keys among them, or of 256, 32 for each of eight wavefronts that look at the same keys (paged_tile_rows says which, and what it measured).
 //   Tiles of 256 are bound by the issue of vector and matrix instructions together, which share a SIMD's time (measured: a 32x32 product keeps
@@ -44,6 +44,7 @@ constexpr int kStageBlocks = 4;  // blocks of code rows that such a workgroup ex
 constexpr float kNoScore = -1.0e30f;   // score of a row that takes no part, reference of a column without scores
 constexpr float kRaiseAt = 15.0f;      // a score may exceed the reference by this (2^15 is the largest weight) ...
 constexpr float kRaiseTo = 7.0f;       // ... and then gets a reference this far below it
+constexpr float kApartFactor = 1.0f + 1.5f / 4096, kApart = 5.2823399e-4f;  // half a step of binary16, 2^-12 to 2^-11 of a number, and its base-2 logarithm
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
@@ -67,6 +68,8 @@ __device__ __forceinline__ Halves neighbours(float v) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return {__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
+// The value of lane l ^ 8.
+__device__ __forceinline__ float other_eight(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, false)); }  // row_ror:8
 __device__ __forceinline__ float halves_max(float v) {
   const Halves h = halves(v);
   return fmaxf(h.lo, h.hi);
@@ -425,7 +428,13 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
   if (wg_row >= rows) return;                                   // whole workgroup
   const int row0 = wg_row + wr * W;                             // first row of the wavefront
   const bool idle = row0 >= rows;                               // (of a workgroup whose wavefronts have rows of their own)
-  const int my_row = min(row0 + col, rows - 1), my_token = my_row / R;
+  // Up to eight rows in a tile of 16 (a generated token of every sequence): each in two columns, whose weights are half a step of binary16
+  // apart, so that their roundings differ and half as much is left in the sum of both: 1.1e-4 of a weight, 2.1e-4 of one column.  Outputs are off by
+  // 2.4e-4 of their norm in place of 2.9e-4 (2.1e-4 is their own rounding), for 0.25 us of a call over 640 rows and 1 % of long ones.  (The
+  // second column for what the first one's rounding drops would leave 2.1e-4, and takes 6 to 17 %.)
+  const bool twice = W == 16 && rows - wg_row <= 8;
+  auto apart = [&] { return twice && (lane & 8) ? kApart : 0.0f; };
+  const int my_row = min(row0 + (twice ? col & 7 : col), rows - 1), my_token = my_row / R;
   const float sm2 = a.sm_scale * kLog2e;
 
   const uint16_t *q_at = a.q + (s.first + my_token) * a.q_stride + (head * R + my_row - my_token * R) * kD + 8 * g_lane;
@@ -511,7 +520,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
     };
     (top_of(y), ...);
     if (__builtin_expect(__ballot(top > limit) != 0ull, 0)) {
-      const float all = T::column_max(top);
+      float all = T::column_max(top);
+      if (W == 16 && twice) all = fmaxf(all, other_eight(all));  // (one reference for both columns)
       float by = 0.0f;
       if (all > limit) {  // the lanes of a column agree
         const float to = rintf(m + all) - kRaiseTo;
@@ -700,7 +710,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       sum[0] *= u;
       sum[1] *= u;
       const float s0 = T::column_sum(NG == 2 ? sum[0] : sum[0] + sum[1]);
-      start[0] = start_slots(g_lane == 0 ? s0 : 0.0f, g_lane == 0 ? 0x3F803F80u : g_lane == 1 ? 0x00003F80u : 0u);
+      start[0] = start_slots(g_lane == 0 ? s0 : g_lane == 1 ? apart() : 0.0f, g_lane == 0 ? 0x3F803F80u : g_lane == 1 ? 0x00003F80u : 0u);
       if constexpr (NG == 2) {
         const float s1 = T::column_sum(sum[1]);
         start[1] = start_slots(g_lane == 0 ? s1 : 0.0f, 0u);
@@ -744,7 +754,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       raise([&](float alpha) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) acc_z[g] *= alpha;
-        if (g_lane == 1) start[0] = start_slots(-m, 0x00003F80u);
+        if (g_lane == 1) start[0] = start_slots(apart() - m, 0x00003F80u);
       }, y...);
     };
     // weights of a block's scores, and their sum
@@ -1080,7 +1090,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       float y[NY];
       score16(y, key, [&](u32x4 k, int at, Acc acc) { return T::bf16(k, q_hi[at], T::bf16(k, q_lo[at], acc)); });
 #pragma unroll
-      for (int i = 0; i < NY; ++i) y[i] = blk * 32 + row_of(i) < wide ? y[i] - m : kNoScore;
+      for (int i = 0; i < NY; ++i) y[i] = blk * 32 + row_of(i) < wide ? y[i] + (apart() - m) : kNoScore;
       weigh(y);
 #pragma unroll
       for (int i = 0; i < NY; ++i) l += y[i];
@@ -1150,13 +1160,24 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
     }
   }
 
+  // (of a tile of 16) the sum of a row's two columns
+  [[maybe_unused]] auto both = [&](float x) { return x + other_eight(x); };
+  [[maybe_unused]] auto join_columns = [&](float &sum) {
+    if (!twice) return;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[j][i] = both(o[j][i]);
+    sum = both(sum);
+  };
   if constexpr (kMergeFirst) {
+    float sum = T::column_sum(l);
+    join_columns(sum);
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       *reinterpret_cast<f32x4 *>(&sh.own[wk].o[col][T::channel(j, 0, g_lane)]) = (f32x4){o[j][0], o[j][1], o[j][2], o[j][3]};
       o[j] = T::zero();
     }
-    const float sum = T::column_sum(l);
     if (g_lane == 0) {
       sh.m[wk][col] = limit < 0.0f ? kNoScore : m;
       sh.l[wk][col] = sum;
@@ -1178,7 +1199,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       float y[NY];
       score16(y, key, [&](u32x4 k, int at, Acc acc) { return T::f16(k, raw[at], acc); });
 #pragma unroll
-      for (int i = 0; i < NY; ++i) y[i] = __builtin_fmaf(y[i], sm2, -m);
+      for (int i = 0; i < NY; ++i) y[i] = __builtin_fmaf(y[i], sm2, apart() - m);
       if (blk * 32 + 31 > low_token) {  // uniform over the wavefront: some row may not look at all of the block
 #pragma unroll
         for (int i = 0; i < NY; ++i)
@@ -1274,6 +1295,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
   } else if constexpr (kMergeFirst) {
     const bool with_self = group_begin <= self_at && run_start(split * WK + WK) > self_at;  // uniform: this workgroup has the chunk's block
     if (self_begin < self_end) {
+      join_columns(l);
 #pragma unroll
       for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x4 *>(&sh.self[col][T::channel(j, 0, g_lane)]) = part_of(j, 0);
       if (g_lane == 0) { sh.m[WK][col] = m; sh.l[WK][col] = l; }
@@ -1284,13 +1306,14 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
     const int r = threadIdx.x >> 4, i = threadIdx.x & 15;
     const int i1 = i ^ ((i & 8) ? 15 : 0), i2 = i1 ^ ((i1 & 4) ? 7 : 0), place = (i & 8) | (i1 & 4) | (i2 & 3), ch = 8 * place;
     float top = sh.m[0][r], sum = 0.0f, x[8];
+    const float once = twice ? 1.0f / (1.0f + kApartFactor) : 1.0f;
 #pragma unroll
     for (int w = 1; w < WK; ++w) top = fmaxf(top, sh.m[w][r]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = 0.0f;
 #pragma unroll
     for (int w = 0; w < WK; ++w) {
-      const float f = exp2_bare(sh.m[w][r] - top);
+      const float f = exp2_bare(sh.m[w][r] - top) * once;
       sum += f * sh.l[w][r];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] += f * sh.own[w].o[r][ch + e];
@@ -1315,7 +1338,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 ? 3 :
       for (int e = 0; e < 8; ++e) x[e] *= inv_sqrt128();
     }
     if (with_self) {
-      const float self_m = sh.m[WK][r], all = fmaxf(top, self_m), f = exp2_bare(top - all), g = exp2_bare(self_m - all);
+      const float self_m = sh.m[WK][r], all = fmaxf(top, self_m), f = exp2_bare(top - all), g = exp2_bare(self_m - all) * once;
       sum = f * sum + g * sh.l[WK][r];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = f * x[e] + g * sh.self[r][ch + e];
