@@ -331,6 +331,11 @@ int64_t positions(const at::Tensor &pos, int64_t rows, int axes) {
   need(rows <= 1 || pos.stride(-1) == 1, "positions: the rows of an axis have to lie next to each other");
   return pos.dim() == 2 && pos.size(0) > 1 ? pos.stride(0) : rows;
 }
+uint32_t flags_of(PyObject *o) {
+  const long flags = integer(o);
+  need(flags >= 0 && flags <= (long)UINT32_MAX, "flags do not fit 32 bits");
+  return (uint32_t)flags;
+}
 int count(int64_t n, const char *what) {
   need(n >= 0 && n <= INT32_MAX, what, " does not fit 32 bits");
   return (int)n;
@@ -491,11 +496,11 @@ PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]), &row_start = tensor(a[3]);
     const int64_t ks = packed(k, "k", -1, pages.c.Hkv), rows = k.size(0), vs = packed(v, "v", rows, pages.c.Hkv);
     const akvq_chunk chunk = chunk_of(pages, row_start, rows, a[4]);
+    const float clip = (float)number(a[5]);
+    const uint32_t flags = flags_of(a[6]);
     Here here;
     for (const at::Tensor *t : {&k, &v, &row_start}) here(*t);
     pages.on(a[0], here);
-    const float clip = (float)number(a[5]);
-    const uint32_t flags = (uint32_t)integer(a[6]);
     int status = 0;
     if (rows > 0) {
       void *const stream = here.stream();
@@ -529,14 +534,14 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const at::Tensor lse = a[10] == Py_None ? at::Tensor() : tensor(a[10]);
     need(!lse.defined() || (lse.scalar_type() == at::kFloat && lse.is_contiguous() && lse.dim() == 2 && lse.size(0) == rows && lse.size(1) == Hq),
          "lse has to be fp32 [rows, Hq]");
+    const float sm_scale = (float)number(a[6]);
+    const long asked = integer(a[7]);
+    const uint32_t flags = flags_of(a[8]);
     Here here;
     for (const at::Tensor *t : {&q, &k, &v, &row_start, &out}) here(*t);
     if (lse.defined()) here(lse);
     pages.on(a[0], here);
     void *const lse_at = lse.defined() ? lse.data_ptr() : nullptr;
-    const float sm_scale = (float)number(a[6]);
-    const long asked = integer(a[7]);
-    const uint32_t flags = (uint32_t)integer(a[8]);
     int status = 0;
     if (rows > 0) {
       const int n_split = asked > 0 ? (int)std::min<long>(asked, INT32_MAX)
