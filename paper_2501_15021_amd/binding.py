@@ -282,10 +282,11 @@ def select_salient(cache: Cache, mode: int, *, is_text: Optional[torch.Tensor] =
         assert q_tail.is_contiguous() and k.is_contiguous()
         B, Hq, W, _ = q_tail.shape
         T = k.shape[2]
+        assert B == cache.B and q_tail.shape[3] == D and k.shape == (B, cache.Hkv, T, D)  # of all the cache's sequences
         nws = lib().akvq_select_workspace_bytes(B, Hq, cache.Hkv, T, W)
         ws = cache.workspace("select", nws)
         if mass_out is not None:
-            assert mass_out.dtype == torch.float32 and mass_out.is_contiguous()
+            assert mass_out.dtype == torch.float32 and mass_out.is_contiguous() and mass_out.numel() >= B * cache.Hkv * T
         st = lib().akvq_select_salient(C.byref(c), mode, None, _ptr(q_tail), Hq, _ptr(k), T, W, top_k, sm_scale,
                                        _ptr(mass_out), _ptr(ws), ws.numel(), _stream())
     _check(st, "akvq_select_salient")
