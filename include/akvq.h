@@ -322,7 +322,11 @@ int akvq_rope_axes_table(const akvq_axes *axes, const int32_t *pos, int64_t pos_
  *     lies behind it takes no part in attention); it sizes that call's launches and workspaces, so one bound for many steps keeps a
  *     captured call valid.  Where rows are written goes by seq_len alone.
  *   The 16-bit rows are the sequences' own, as in akvq_cache: k_sal, v_sal, sal_idx [B][Hkv][S_cap] (positions of the sequence,
- *     ascending), sal_cnt [B][Hkv].
+ *     ascending), sal_cnt [B][Hkv].  The bit that marks a listed row lies in its page: sequences may share pages that nobody writes to any more
+ *     only where their lists agree on the rows of these pages, and each needs the 16-bit rows in its own arrays (the caller copies them).
+ *     akvq_select_salient writes the lists of all B sequences for one prompt length.  Lists of prompts of unequal length, of a prompt that
+ *     comes in pieces (final before its first row is written) or of one sequence of a running batch are the caller's to put in place, for
+ *     instance from a selection into arrays of their own.
  *   max_pages * page_rows must stay below 2^30.  table, seq_len and row_start need 4-byte alignment only.
  * The new rows of a call (see "Chunks"): rows [row_start[b], row_start[b + 1]) belong to sequence b; row_start: device, [B + 1] int32,
  *   ascending; n_rows: rows of the arrays; max_rows: an upper bound of the rows of one sequence (what exceeds it takes no part).
@@ -360,7 +364,7 @@ int akvq_paged_append(const akvq_paged *c, const akvq_chunk *rows, const void *k
  *   chunk's rows j <= i of the same sequence, which count as they arrive (binary16), whether or not akvq_paged_append has already
  *   stored them behind seq_len.  One row a sequence is the decode step of a batch of unequal lengths; nothing cached is a first chunk.
  *   q, k, v: post-RoPE, un-rotated.  out: [n_rows][Hq][128] binary16, rows out_stride elements apart.  lse_out: optional, [n_rows][Hq]
- *   fp32.  Hq / Hkv at most 8, max_rows * Hq / Hkv below 2^24 - 256.  fp32 scores, sums and accumulators; the cached rows' queries as
+ *   fp32.  Hq / Hkv at most 8, max_rows * Hq / Hkv at most 2^24 - 256.  fp32 scores, sums and accumulators; the cached rows' queries as
  *   integers of 20 bits (16 against 16-bit rows), weights of 11 bits (16 for the 16-bit rows), cached values as they are (with G = 64 and
  *   hundreds of rows a sequence rounded to 11 bits once).
  *   Rows listed as salient are read from the overlay whatever their page.  NaN or infinity in a sequence's own rows gives

@@ -460,7 +460,12 @@ class PagedCache:
     The caller owns the page table: it writes page numbers into table [B, max_pages] (-1: no page) and advances seq_len [B], both int32
     on the device, so that calls can be captured and replayed while they change.  max_len is what the host knows of the longest
     sequence (by default all that the table can name): it sizes attention's launches, and rows behind it take no part there;
-    paged_append stores rows at seq_len whatever it is.  select_salient takes a PagedCache, too."""
+    paged_append stores rows at seq_len whatever it is.
+
+    select_salient takes a PagedCache, too, and writes the lists of all its sequences, for prompts of one length that are there whole.  For
+    prompts of unequal length, in pieces, or for one sequence of a running batch the caller copies lists into sal_idx[b] and counts()[b], for
+    instance from a selection into a Cache of its own, before the first row is appended.  Sequences may share pages that nobody writes to any
+    more where their lists agree on the rows of these pages and k_sal, v_sal hold the listed rows for each."""
 
     def __init__(self, B: int, Hkv: int, G: int, n_pages: int, max_pages: int, page_rows: int = 64, S_cap: int = 64, device="cuda",
                  fill: Optional[int] = None):
@@ -514,7 +519,8 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torc
                     lse: Optional[torch.Tensor] = None) -> torch.Tensor:
     """akvq_paged_attention: a chunk's rows q [n, Hq, 128], k and v [n, Hkv, 128] fp16 (row_start and max_rows as in paged_append) over the
     cached rows of their sequences and over the chunk's own rows up to each.  Returns out [n, Hq, 128] fp16; lse [n, Hq] fp32 is
-    written where given.  Rows that belong to no sequence are left as they are.  The workspace is of its own for every call: calls on two
+    written where given.  Rows that belong to no sequence, or lie behind max_rows of one, are left as they are: without out= they hold
+    whatever was there.  out may not overlap q, k or v.  The workspace is of its own for every call: calls on two
     streams, or two captured graphs, share none."""
     st, out = (_native or native()).paged_attention(cache, q, k, v, row_start, max_rows, sm_scale, n_split, flags, out, lse)
     if st:
