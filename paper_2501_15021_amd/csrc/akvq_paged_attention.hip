@@ -24,12 +24,12 @@
 //   Tiles of 256 are bound by the issue of vector and matrix instructions together, which share a SIMD's time (measured: a 32x32 product keeps
 // the vector unit for 15 of its 33 cycles, a 16x16 one for 12 of 19, a vector instruction takes 3 to 4, an exponential 9), and by the power that
 // matrix instructions may take (the 17 products of a block alone, on random data, take 0.9 ms of what follows).  So every block is expanded once
-// for all eight.  4 x 2048 rows of 32 heads over 8192 cached ones: 1.25-1.3 ms, 960-1000 TFLOP/s of what the formula takes (a 16-bit
-// matrix product of 8192 x 8192 x 8192: 1268); first chunks of 4096, which LDS reads bind as much, 0.28 ms, 780.
+// for all eight.  4 x 2048 rows of 32 heads over 8192 cached ones: 1.23-1.3 ms, 955-1010 TFLOP/s of what the formula takes (a 16-bit
+// matrix product of 8192 x 8192 x 8192: 1268); first chunks of 4096, which LDS reads bind as much, 0.27-0.29 ms, 760-805.
 //   Tiles of 16 and 32 read the cache with what their wavefronts have under way.  One row of 4 heads over 32768 rows of 128 units (G = 64):
-// 94-97 us, 3.6 TB/s, where vector instructions take 63 % of the time and matrix instructions 27; one row over 2048 to 4096 rows of 512 units 36 us, 3.2
-// TB/s, 13 of it before the first block and behind the last: two wavefronts a SIMD, 42 and 14 %.  One row over 640 of 32 units: 8.0 us and 2.8
-// for the merge, a chain of memory round trips.
+// 94-99 us, 3.4-3.6 TB/s, where vector instructions take 62 % of the time and matrix instructions 26; one row over 2048 to 4096 rows of 512 units
+// 35-37 us, 3.1 TB/s, 13 of it before the first block and behind the last: two wavefronts a SIMD, 43 and 14 %.  One row over 640 of 32 units: 8.2 us
+// and 2.8 for the merge, a chain of memory round trips.
 #include "akvq_device.h"
 #include "akvq_kernels.h"
 
