@@ -55,7 +55,7 @@ def _equal_weights(G, zeros, scales):
 
 
 @pytest.mark.parametrize("G", [128, 64])
-@pytest.mark.parametrize("zeros", [[1, -5, 300, -1000, 7], [1023, 1024, 1025, 1026, 1027], [-1021, -1024, -1025, -2045, -2047], [2047, 2048, 2049, 3071, 3072],
+@pytest.mark.parametrize("zeros", [[1, -5, 300, -1000, 7], [1023, 1024, 1025, 1026, 1027], [-1021, -1024, -1025, -2045, -2047], [2047, 2048, 2049, 3583, 3584],
                                    [4095, -4096, 10000, -20001, 12345], [32767, -32768, 1025, -32767, 31743]])
 def test_zero_points_are_exact(zeros, G):
     _equal_weights(G, zeros, (2.0 ** -6, 2.0 ** -7))
