@@ -381,6 +381,61 @@ int akvq_paged_attention(const akvq_paged *c, const akvq_chunk *rows, const void
                          float *lse_out, int n_split, void *workspace, size_t workspace_bytes, uint32_t flags, void *stream);
 
 /*
+ * Pages of 4-bit codes: the cache in pages with the 4 bits a channel of Section III-C.1's text tier for every row (Eq. 3-6 with 15
+ *   levels, the scale stored as binary16 rounded up), for layers or models that 2 bits cost too much.  akvq_paged as above, but a block of 32
+ *   rows has 512 words:
+ *     k_codes, v_codes [n_pages][Hkv][page_rows/32][512 words]; meta words, 16-bit rows, lists, table and lengths as above.
+ *       keys, row r of its block, channel e: m=e/32, j=(e%32)/8, i=e%8: word = r/16*256 + (16*j + r%16)*4 + m;  bits [4i, 4i+4).
+ *       values: half=r/16, q=(r%16)/4, ii=r%4, nb=e/16, n=e%16: word = nb%2*256 + (16*q + n)*4 + nb/2;  bits [16*half + 4*ii, +4).
+ *   akvq_paged_nibble_bytes, akvq_paged_nibble_append, akvq_paged_nibble_default_splits, akvq_paged_nibble_attention: as the calls without "nibble", their arguments,
+ *   refusals and what they promise of rows, pages, lengths and lists among it, over such pools; workspaces are sized by
+ *   akvq_paged_workspace_bytes.  A cache that one kind of call has written means nothing to the other kind.
+ *   Scores of cached rows: the query as an integer of 20 bits, codes as they are.  Weights have 11 bits, cached values as with 2 bits.
+ */
+int akvq_paged_nibble_bytes(const akvq_paged *shape, size_t out_bytes[8]);
+int akvq_paged_nibble_append(const akvq_paged *c, const akvq_chunk *rows, const void *k, int64_t k_stride, const void *v,
+                       int64_t v_stride, float clip, uint32_t flags, void *stream);
+int akvq_paged_nibble_default_splits(const akvq_paged *c, int Hq, int max_rows);
+int akvq_paged_nibble_attention(const akvq_paged *c, const akvq_chunk *rows, const void *q, int64_t q_stride, int Hq, const void *k,
+                          int64_t k_stride, const void *v, int64_t v_stride, float sm_scale, void *out, int64_t out_stride,
+                          float *lse_out, int n_split, void *workspace, size_t workspace_bytes, uint32_t flags, void *stream);
+
+/*
+ * akvq_rotary_rows -- rotary positions in either layout, of the whole head or its first channels, with a magnitude (what models stretched to
+ *   long contexts multiply sine and cosine by): pair i < dim / 2 of a row turns by pos[axis[i]][row] * inv_freq[i].  A pair is channels i and
+ *   i + dim / 2 (AKVQ_ROTARY_HALF) or 2i and 2i + 1 (AKVQ_ROTARY_INTERLEAVED); channels from dim on stay as they are, bit for bit.
+ *     c = magnitude * cos, s = magnitude * sin, each rounded once to 32 bits from an angle that is formed in 64;
+ *     (x, y) -> (x c - y s, y c + x s): the second product is rounded to 32 bits, its sum with the first once, that to binary16.
+ *   flags: AKVQ_ROPE_INVERSE (-s for s: the transposed rotation, which is the gradient; with magnitude 1 it turns the rows back) or 0.
+ *   pos, q, k, q_out, k_out, strides, Hq, Hkv, n_rows: as in akvq_rope_axes.
+ */
+enum { AKVQ_ROTARY_HALF = 0, AKVQ_ROTARY_INTERLEAVED = 1 };
+typedef struct akvq_rotary {
+  int32_t n_axes;     /* 1 to 4 */
+  int32_t layout;     /* AKVQ_ROTARY_* */
+  int32_t dim;        /* channels that turn: a multiple of 16, 16 to 128 */
+  float magnitude;    /* finite */
+  float inv_freq[64]; /* radians per position, of the first dim / 2 pairs: finite (the others are not looked at) */
+  uint8_t axis[64];   /* < n_axes */
+} akvq_rotary;
+int akvq_rotary_rows(const akvq_rotary *rotary, const int32_t *pos, int64_t pos_stride, int n_rows, const void *q, int64_t q_stride,
+                     int Hq, const void *k, int64_t k_stride, int Hkv, void *q_out, int64_t q_out_stride, void *k_out,
+                     int64_t k_out_stride, uint32_t flags, void *stream);
+
+/*
+ * akvq_paged_append_rotary -- a chunk on its way into the cache in one call: queries and keys are turned as akvq_rotary_rows turns them, into
+ *   q_out and k_out (what akvq_paged_attention takes), and the turned keys and the values are written into the pages as akvq_paged_append
+ *   (bits = 2) or akvq_paged_nibble_append (bits = 4) writes them, bit for bit.  pos: one entry for every axis and row of the chunk (pos_stride at
+ *   least rows->n_rows where there are several axes).  Hq = 0: no q.  q_out / k_out may be q / k themselves with the same stride, else they
+ *   overlap none of q, k and v.  Rows that the pages have no place for are turned all the same; rows that belong to no sequence, or lie
+ *   behind max_rows of one, are left alone, in q_out and k_out too.  flags: AKVQ_V_PREROTATED or 0.  n_rows = 0 does nothing.
+ */
+int akvq_paged_append_rotary(const akvq_paged *c, int bits, const akvq_chunk *rows, const akvq_rotary *rotary, const int32_t *pos,
+                             int64_t pos_stride, const void *q, int64_t q_stride, int Hq, const void *k, int64_t k_stride,
+                             const void *v, int64_t v_stride, void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride,
+                             float clip, uint32_t flags, void *stream);
+
+/*
  * akvq_stream_read -- measurement aid, no part of the method: one pass of plain 128-bit loads over src (device, 16-byte
  *   aligned, `bytes` a multiple of 16), nothing computed but an exclusive-or, nothing stored (sink: device, one
  *   uint32, written only if the data happen to fold to a magic value).  non_temporal != 0: the loads carry the

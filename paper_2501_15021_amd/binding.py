@@ -8,6 +8,7 @@ call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional
 
@@ -29,8 +30,11 @@ EXPORTS = ["akvq_strerror", "akvq_last_hip_error", "akvq_version", "akvq_cache_b
            "akvq_decode_static_scratch_bytes", "akvq_decode_attention_static",
            "akvq_massive_workspace_bytes", "akvq_select_massive", "akvq_fold_hadamard", "akvq_stream_read",
            "akvq_rope_axes", "akvq_rope_axes_table", "akvq_paged_bytes", "akvq_paged_append",
-           "akvq_paged_workspace_bytes", "akvq_paged_default_splits", "akvq_paged_attention"]
+           "akvq_paged_workspace_bytes", "akvq_paged_default_splits", "akvq_paged_attention",
+           "akvq_paged_nibble_bytes", "akvq_paged_nibble_append", "akvq_paged_nibble_default_splits", "akvq_paged_nibble_attention",
+           "akvq_rotary_rows", "akvq_paged_append_rotary"]
 TIER_2BIT, TIER_4BIT_COARSE, TIER_4BIT_FINE, TIER_PAD = 0, 1, 2, 3
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 
 
 class AkvqError(RuntimeError):
@@ -47,6 +51,11 @@ class akvq_rope(C.Structure):
 
 class akvq_axes(C.Structure):
     _fields_ = [("n_axes", C.c_int32), ("inv_freq", C.c_float * 64), ("axis", C.c_uint8 * 64)]
+
+
+class akvq_rotary(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("layout", C.c_int32), ("dim", C.c_int32), ("magnitude", C.c_float),
+                ("inv_freq", C.c_float * 64), ("axis", C.c_uint8 * 64)]
 
 
 class akvq_cache(C.Structure):
@@ -157,6 +166,17 @@ def lib() -> C.CDLL:
         L.akvq_paged_attention.argtypes = [C.POINTER(akvq_paged), C.POINTER(akvq_chunk), C.c_void_p, C.c_int64, C.c_int, C.c_void_p,
                                            C.c_int64, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_int,
                                            C.c_void_p, C.c_size_t, C.c_uint32, C.c_void_p]
+        L.akvq_paged_nibble_bytes.restype, L.akvq_paged_nibble_bytes.argtypes = L.akvq_paged_bytes.restype, L.akvq_paged_bytes.argtypes
+        L.akvq_paged_nibble_append.restype, L.akvq_paged_nibble_append.argtypes = L.akvq_paged_append.restype, L.akvq_paged_append.argtypes
+        L.akvq_paged_nibble_default_splits.restype = C.c_int
+        L.akvq_paged_nibble_default_splits.argtypes = L.akvq_paged_default_splits.argtypes
+        L.akvq_paged_nibble_attention.restype, L.akvq_paged_nibble_attention.argtypes = C.c_int, L.akvq_paged_attention.argtypes
+        L.akvq_rotary_rows.restype = C.c_int
+        L.akvq_rotary_rows.argtypes = [C.POINTER(akvq_rotary), *L.akvq_rope_axes.argtypes[1:]]
+        L.akvq_paged_append_rotary.restype = C.c_int
+        L.akvq_paged_append_rotary.argtypes = [C.POINTER(akvq_paged), C.c_int, C.POINTER(akvq_chunk), C.POINTER(akvq_rotary), C.c_void_p,
+                                               C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                               C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_float, C.c_uint32, C.c_void_p]
         _lib = L
     return _lib
 
@@ -453,6 +473,57 @@ def rope_axes_table(axes: RopeAxes, pos: torch.Tensor):
     return table
 
 
+class Rotary:
+    """Rotary positions of a head's first `dim` channels: pair i turns by pos[axis[i]] * inv_freq[i] and is multiplied by `magnitude`.  A pair is
+    channels i and i + dim / 2, or (interleaved) 2i and 2i + 1; channels from dim on stay as they are."""
+
+    def __init__(self, inv_freq, axis=None, dim: int = D, interleaved: bool = False, magnitude: float = 1.0):
+        inv_freq = [float(f) for f in inv_freq]
+        _need(dim in range(16, D + 1, 16), "dim has to be a multiple of 16 up to 128")
+        axis = [0] * (dim // 2) if axis is None else [int(a) for a in axis]
+        _need(len(inv_freq) == dim // 2 and len(axis) == dim // 2, "dim / 2 channel pairs have a frequency and an axis each")
+        _need(min(axis) >= 0 and max(axis) < 4, "axes are 0 to 3")
+        self.dim, self.n_axes = dim, max(axis) + 1
+        self._struct = akvq_rotary(self.n_axes, ROTARY_INTERLEAVED if interleaved else ROTARY_HALF, dim, magnitude,
+                                   (C.c_float * 64)(*inv_freq), (C.c_uint8 * 64)(*axis))
+
+    @classmethod
+    def plain(cls, theta: float, dim: int = D, interleaved: bool = False) -> "Rotary":
+        """inv_freq[i] = theta ** (-2 i / dim)."""
+        return cls([theta ** (-2 * i / dim) for i in range(dim // 2)], None, dim, interleaved)
+
+    @classmethod
+    def linear(cls, theta: float, factor: float, dim: int = D, interleaved: bool = False) -> "Rotary":
+        """Positions interpolated (arXiv 2306.15595): every frequency divided by `factor`."""
+        _need(factor >= 1, "factor has to be at least 1")
+        return cls([theta ** (-2 * i / dim) / factor for i in range(dim // 2)], None, dim, interleaved)
+
+    @classmethod
+    def yarn(cls, theta: float, factor: float, trained: int, dim: int = D, interleaved: bool = False, fast: float = 32.0, slow: float = 1.0,
+             magnitude: Optional[float] = None) -> "Rotary":
+        """A context of `trained` positions stretched `factor` times (arXiv 2309.00071): frequencies that turn less than `slow` times in it
+        are divided by factor, those that turn more than `fast` times stay, those between are blended by their turns; magnitude
+        0.1 ln(factor) + 1 unless given."""
+        _need(factor >= 1 and fast > slow >= 0 and trained > 0, "factor has to be at least 1, fast above slow, trained positive")
+        freq = []
+        for i in range(dim // 2):
+            f = theta ** (-2 * i / dim)
+            keep = min(max((trained * f / (2 * math.pi) - slow) / (fast - slow), 0.0), 1.0)
+            freq.append(f * keep + f / factor * (1 - keep))
+        return cls(freq, None, dim, interleaved, 0.1 * math.log(factor) + 1.0 if magnitude is None else magnitude)
+
+
+def rotary_rows(rotary: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None,
+                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False):
+    """akvq_rotary_rows: rotary positions of a chunk's rows, as rope_axes, in either layout, of part of the head or all of it.  inverse: the
+    transposed rotation, which is the gradient (with magnitude 1 it turns back); the call records none itself and refuses rows that ask
+    for one.  Returns (q_out, k_out)."""
+    st, outs = (_native or native()).rotary_rows(rotary._struct, pos, q, k, q_out, k_out, inverse)
+    if st:
+        _check(st, "akvq_rotary_rows")
+    return outs
+
+
 class PagedCache:
     """One layer's cache in pages: pools that sequences of any lengths share, and for every sequence a row of the page table, its
     number of cached rows and its 16-bit rows.
@@ -465,19 +536,23 @@ class PagedCache:
     select_salient takes a PagedCache, too, and writes the lists of all its sequences, for prompts of one length that are there whole.  For
     prompts of unequal length, in pieces, or for one sequence of a running batch the caller copies lists into sal_idx[b] and counts()[b], for
     instance from a selection into a Cache of its own, before the first row is appended.  Sequences may share pages that nobody writes to any
-    more where their lists agree on the rows of these pages and k_sal, v_sal hold the listed rows for each."""
+    more where their lists agree on the rows of these pages and k_sal, v_sal hold the listed rows for each.
+
+    bits: of a code, 2 or 4; paged_append, paged_append_rotary and paged_attention go by it."""
 
     def __init__(self, B: int, Hkv: int, G: int, n_pages: int, max_pages: int, page_rows: int = 64, S_cap: int = 64, device="cuda",
-                 fill: Optional[int] = None):
-        self.B, self.Hkv, self.G, self.page_rows = B, Hkv, G, page_rows
+                 fill: Optional[int] = None, bits: int = 2):
+        _need(bits in (2, 4), "codes have 2 or 4 bits")
+        self.B, self.Hkv, self.G, self.page_rows, self.bits = B, Hkv, G, page_rows, bits
         self.n_pages, self.max_pages, self.S_cap, self.max_len = n_pages, max_pages, S_cap, max_pages * page_rows
         sizes = (C.c_size_t * 8)()
-        _check(lib().akvq_paged_bytes(C.byref(akvq_paged(B, Hkv, G, page_rows, n_pages, max_pages, S_cap, 0)), sizes), "akvq_paged_bytes")
+        bytes_of = lib().akvq_paged_bytes if bits == 2 else lib().akvq_paged_nibble_bytes
+        _check(bytes_of(C.byref(akvq_paged(B, Hkv, G, page_rows, n_pages, max_pages, S_cap, 0)), sizes), bytes_of.__name__)
         dev = torch.device(device)
         mk = (lambda n: torch.empty(n, dtype=torch.uint8, device=dev)) if fill is None else \
              (lambda n: torch.full((n,), fill, dtype=torch.uint8, device=dev))
-        self.k_codes = mk(sizes[0]).view(torch.int32).view(n_pages, Hkv, page_rows // 32, 256)
-        self.v_codes = mk(sizes[1]).view(torch.int32).view(n_pages, Hkv, page_rows // 32, 256)
+        self.k_codes = mk(sizes[0]).view(torch.int32).view(n_pages, Hkv, page_rows // 32, 128 * bits)
+        self.v_codes = mk(sizes[1]).view(torch.int32).view(n_pages, Hkv, page_rows // 32, 128 * bits)
         self.k_meta = mk(sizes[2]).view(torch.int32).view(n_pages, Hkv, page_rows, D // G)
         self.v_meta = mk(sizes[3]).view(torch.int32).view(n_pages, Hkv, page_rows, D // G)
         self.k_sal = torch.zeros(sizes[4] // 2, dtype=torch.int16, device=dev).view(B, Hkv, S_cap, D)
@@ -507,17 +582,30 @@ _PLAIN_PAGED = PagedCache.paged_struct  # as _PLAIN
 
 def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int, clip: float,
                  flags: int = 0) -> None:
-    """akvq_paged_append: rows k, v [n, Hkv, 128] fp16 of a chunk, row_start[b] to row_start[b + 1] those of sequence b (max_rows at
+    """akvq_paged_append (akvq_paged_nibble_append for a cache of 4-bit codes): rows k, v [n, Hkv, 128] fp16 of a chunk, row_start[b] to row_start[b + 1] those of sequence b (max_rows at
     most), become its cache rows from seq_len[b] on.  cache.seq_len is the caller's to advance."""
     st = (_native or native()).paged_append(cache, k, v, row_start, max_rows, clip, flags)
     if st:
         _check(st, "akvq_paged_append")
 
 
+def paged_append_rotary(cache: PagedCache, rotary: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                        row_start: torch.Tensor, max_rows: int, clip: float, q_out: Optional[torch.Tensor] = None,
+                        k_out: Optional[torch.Tensor] = None, flags: int = 0):
+    """akvq_paged_append_rotary: a chunk's queries (q may be None) and keys are turned as rotary_rows turns them, into q_out and k_out (new
+    tensors where None; q and k themselves turn in place), and the turned keys and v become cache rows as paged_append writes them, in one
+    call.  pos [axes, n] int32.  Rows that belong to no sequence, or lie behind max_rows of one, are left as they are, in q_out and k_out
+    too: new tensors hold whatever was there.  cache.seq_len is the caller's to advance.  Returns (q_out, k_out), for paged_attention."""
+    st, outs = (_native or native()).paged_append_rotary(cache, rotary._struct, pos, q, k, v, row_start, max_rows, clip, q_out, k_out, flags)
+    if st:
+        _check(st, "akvq_paged_append_rotary")
+    return outs
+
+
 def paged_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int,
                     sm_scale: float, n_split: int = 0, flags: int = 0, out: Optional[torch.Tensor] = None,
                     lse: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """akvq_paged_attention: a chunk's rows q [n, Hq, 128], k and v [n, Hkv, 128] fp16 (row_start and max_rows as in paged_append) over the
+    """akvq_paged_attention (akvq_paged_nibble_attention for a cache of 4-bit codes): a chunk's rows q [n, Hq, 128], k and v [n, Hkv, 128] fp16 (row_start and max_rows as in paged_append) over the
     cached rows of their sequences and over the chunk's own rows up to each.  Returns out [n, Hq, 128] fp16; lse [n, Hq] fp32 is
     written where given.  Rows that belong to no sequence, or lie behind max_rows of one, are left as they are: without out= they hold
     whatever was there.  out may not overlap q, k or v.  The workspace is of its own for every call: calls on two

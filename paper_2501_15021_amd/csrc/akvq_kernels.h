@@ -474,6 +474,39 @@ inline int paged_splits(long units, long tokens, long R, long len) {
   return (int)paged_tile_splits(paged_tile_rows(units, tokens, R, len), units, tokens, R, len);
 }
 
+// ---- pages of 4-bit codes: the same calls over pools of twice the words (akvq_paged4.hip, akvq_paged4_attention.hip) ----
+hipError_t launch_paged4_append(const PagedAppendArgs &a, int G, hipStream_t stream);
+hipError_t launch_paged4_attention(const PagedAttentionArgs &a, int G, hipStream_t stream);
+
+// ---- rotary positions in either layout, and on the way into the pages (akvq_rotary.hip, akvq_paged_turn.hip) ----
+// Pair i < dim / 2 of a row (channels i, i + dim / 2, or 2i, 2i + 1) turns by pos[axis[i]][row] * inv_freq[i], and is multiplied by magnitude.
+struct RotaryPlan {
+  float inv_freq[64];
+  uint8_t axis[64];
+  const int32_t *pos;
+  long long pos_stride;
+  float magnitude;
+  int dim, interleaved, inverse;
+};
+struct RotaryArgs {
+  RotaryPlan plan;
+  int n_rows, Hq, Hkv;
+  const uint16_t *q, *k;
+  uint16_t *q_out, *k_out;
+  long long q_stride, k_stride, q_out_stride, k_out_stride;
+  int heads_per_wave;  // (set by the launcher)
+};
+hipError_t launch_rotary_rows(RotaryArgs a, hipStream_t stream);
+struct PagedTurnArgs {
+  PagedAppendArgs append;  // (k: not yet turned)
+  RotaryPlan plan;
+  const uint16_t *q;
+  uint16_t *q_out, *k_out;
+  long long q_stride, q_out_stride, k_out_stride;
+  int Hq;
+};
+hipError_t launch_paged_turn(const PagedTurnArgs &a, int G, int bits, hipStream_t stream);
+
 // status of a launch for the C ABI; keeps a failed launch's code for akvq_last_hip_error (akvq_api.hip)
 int launch_status(hipError_t e);
 

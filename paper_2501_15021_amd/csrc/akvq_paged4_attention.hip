@@ -1,0 +1,6 @@
+// Attention of a chunk over pages of 4-bit codes (akvq_paged_attention.h).
+#include "akvq_paged_attention.h"
+
+namespace akvq {
+hipError_t launch_paged4_attention(const PagedAttentionArgs &a, int G, hipStream_t stream) { return launch_attention<4>(a, G, stream); }
+}  // namespace akvq

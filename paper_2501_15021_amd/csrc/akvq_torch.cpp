@@ -27,7 +27,7 @@ constexpr int64_t kHeadDim = 128;
 struct Names {
   PyObject *B, *Hkv, *G, *T_cap, *S_cap, *T_len, *k_codes, *v_codes, *k_meta, *v_meta, *k_sal, *v_sal, *sal_idx, *sal_cnt,
       *fine_mask, *W, *k_win, *v_win, *workspace, *decode, *struct_, *window_struct,
-      *page_rows, *n_pages, *max_pages, *max_len, *table, *seq_len, *paged_struct;
+      *page_rows, *n_pages, *max_pages, *max_len, *table, *seq_len, *paged_struct, *bits;
 } names;
 // What the package's own cache class describes itself with, and the types of the descriptions (plain_cache).
 struct Plain {
@@ -314,8 +314,9 @@ void no_gradient(const at::Tensor &t, const char *what) {
 }
 at::Tensor fresh(at::IntArrayRef shape, const at::Tensor &like) { return at::empty(shape, like.options().dtype(at::kHalf).requires_grad(false)); }
 
-akvq_axes axes_of(PyObject *o) {  // the description that RopeAxes holds
-  akvq_axes axes;
+template <typename Axes>
+Axes axes_of(PyObject *o) {  // the description that RopeAxes or Rotary holds
+  Axes axes;
   Py_buffer view;
   if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) throw Failed();
   const bool fits = view.len == (Py_ssize_t)sizeof(axes);
@@ -341,45 +342,58 @@ int count(int64_t n, const char *what) {
   return (int)n;
 }
 
-// rope_axes(axes, pos, q, k, q_out, k_out, inverse) -> (status, (q_out, k_out))
-PyObject *rope_axes(PyObject *, PyObject *const *a, Py_ssize_t n) {
+// Rows of a call that turns them: packed rows and where they go, which is a new tensor for None.
+struct Turned {
+  const void *in = nullptr;
+  void *out_at = nullptr;
+  int64_t stride = 0, out_stride = 0;
+  int heads = 0;
+  at::Tensor out;
+  void take(PyObject *in_obj, PyObject *out_obj, const char *what, const char *what_out, int64_t rows, int64_t want_heads) {
+    const at::Tensor &t = tensor(in_obj);
+    stride = packed(t, what, rows, want_heads);
+    out = out_obj == Py_None ? fresh(t.sizes(), t) : tensor(out_obj);
+    out_stride = packed(out, what_out, rows, t.size(1));
+    no_gradient(t, what);
+    no_gradient(out, what_out);
+    in = t.data_ptr();
+    out_at = out.data_ptr();
+    heads = count(t.size(1), "heads");
+  }
+  // a new reference to what the call returns for it
+  PyObject *result(PyObject *in_obj, PyObject *out_obj) const {
+    return in_obj == Py_None ? Py_NewRef(Py_None) : out_obj != Py_None ? Py_NewRef(out_obj) : THPVariable_Wrap(out);
+  }
+};
+
+// (axes, pos, q, k, q_out, k_out, inverse) -> (status, (q_out, k_out)), of rope_axes and rotary_rows
+template <typename Axes, typename Turn>
+PyObject *turn_rows(PyObject *const *a, Py_ssize_t n, const char *name, Turn turn) {
   HANDLE_TH_ERRORS
   if (n != 7) {
-    PyErr_SetString(PyExc_TypeError, "rope_axes takes 7 arguments");
+    PyErr_Format(PyExc_TypeError, "%s takes 7 arguments", name);
     return nullptr;
   }
   try {
     need(a[2] != Py_None || a[3] != Py_None, "neither q nor k");
-    const akvq_axes axes = axes_of(a[0]);
+    const Axes axes = axes_of<Axes>(a[0]);
     const at::Tensor &pos = tensor(a[1]);
     const at::Tensor &lead = tensor(a[2] != Py_None ? a[2] : a[3]);
     need(lead.dim() == 3, a[2] != Py_None ? "q" : "k", " has to be fp16 [rows, heads, 128]");
     const int64_t rows = lead.size(0);
-    struct { const void *in = nullptr; void *out = nullptr; int64_t stride = 0, out_stride = 0; int heads = 0; } x[2];
-    at::Tensor outs[2];
+    Turned x[2];
     static const char *const what[2] = {"q", "k"}, *const what_out[2] = {"q_out", "k_out"}, *const without[2] = {"q_out without q", "k_out without k"};
     for (int i = 0; i < 2; ++i) {
-      if (a[2 + i] == Py_None) {
-        need(a[4 + i] == Py_None, without[i]);
-        continue;
-      }
-      const at::Tensor &t = tensor(a[2 + i]);
-      x[i].stride = packed(t, what[i], rows, -1);
-      outs[i] = a[4 + i] == Py_None ? fresh(t.sizes(), t) : tensor(a[4 + i]);
-      x[i].out_stride = packed(outs[i], what_out[i], rows, t.size(1));
-      no_gradient(t, what[i]);
-      no_gradient(outs[i], what_out[i]);
-      x[i].in = t.data_ptr();
-      x[i].out = outs[i].data_ptr();
-      x[i].heads = count(t.size(1), "heads");
+      if (a[2 + i] == Py_None) need(a[4 + i] == Py_None, without[i]);
+      else x[i].take(a[2 + i], a[4 + i], what[i], what_out[i], rows, -1);
     }
     const int64_t pos_stride = positions(pos, rows, axes.n_axes);
     Here here;
     here(pos);
     for (int i = 0; i < 2; ++i)
-      if (x[i].heads || a[2 + i] != Py_None) {
+      if (a[2 + i] != Py_None) {
         here(tensor(a[2 + i]));
-        here(outs[i]);
+        here(x[i].out);
       }
     const int inverse = PyObject_IsTrue(a[6]);
     if (inverse < 0) return nullptr;
@@ -389,24 +403,22 @@ PyObject *rope_axes(PyObject *, PyObject *const *a, Py_ssize_t n) {
       void *const stream = here.stream();
       const void *const at_pos = pos.data_ptr();
       Py_BEGIN_ALLOW_THREADS
-      status = akvq_rope_axes(&axes, static_cast<const int32_t *>(at_pos), pos_stride, n_rows, x[0].in, x[0].stride, x[0].heads,
-                              x[1].in, x[1].stride, x[1].heads, x[0].out, x[0].out_stride, x[1].out, x[1].out_stride,
-                              inverse ? AKVQ_ROPE_INVERSE : 0, stream);
+      status = turn(&axes, static_cast<const int32_t *>(at_pos), pos_stride, n_rows, x[0].in, x[0].stride, x[0].heads, x[1].in, x[1].stride,
+                    x[1].heads, x[0].out_at, x[0].out_stride, x[1].out_at, x[1].out_stride, inverse ? AKVQ_ROPE_INVERSE : 0, stream);
       Py_END_ALLOW_THREADS
       for (int i = 0; i < 2; ++i)
-        if (a[4 + i] != Py_None) written(outs[i]);
+        if (a[4 + i] != Py_None) written(x[i].out);
     }
-    Held out[2];
-    for (int i = 0; i < 2; ++i) {
-      out[i].p = a[2 + i] == Py_None ? Py_NewRef(Py_None) : a[4 + i] != Py_None ? Py_NewRef(a[4 + i]) : THPVariable_Wrap(outs[i]);
-      if (!out[i].p) return nullptr;
-    }
-    return Py_BuildValue("i(OO)", status, out[0].p, out[1].p);
+    Held q(x[0].result(a[2], a[4])), k(x[1].result(a[3], a[5]));
+    if (!q.p || !k.p) return nullptr;
+    return Py_BuildValue("i(OO)", status, q.p, k.p);
   } catch (const Failed &) {
     return nullptr;
   }
   END_HANDLE_TH_ERRORS
 }
+PyObject *rope_axes(PyObject *, PyObject *const *a, Py_ssize_t n) { return turn_rows<akvq_axes>(a, n, "rope_axes", akvq_rope_axes); }
+PyObject *rotary_rows(PyObject *, PyObject *const *a, Py_ssize_t n) { return turn_rows<akvq_rotary>(a, n, "rotary_rows", akvq_rotary_rows); }
 
 // rope_axes_table(axes, pos) -> (status, (cos, sin))
 PyObject *rope_axes_table(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -416,7 +428,7 @@ PyObject *rope_axes_table(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return nullptr;
   }
   try {
-    const akvq_axes axes = axes_of(a[0]);
+    const akvq_axes axes = axes_of<akvq_axes>(a[0]);
     const at::Tensor &pos = tensor(a[1]);
     need(pos.dim() == 1 || pos.dim() == 2, "positions have to be int32 [axes, rows]");
     const int64_t rows = pos.size(-1), pos_stride = positions(pos, rows, axes.n_axes);
@@ -439,8 +451,9 @@ PyObject *rope_axes_table(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // The cache's description, and the device of its pools.
 struct Pages {
   akvq_paged c;
+  int bits;   // of a code
   Held held;  // keeps what the pointers come from
-  Pages(PyObject *cache) {
+  Pages(PyObject *cache) : bits(bits_of(cache)) {
     if (described(cache, names.paged_struct, paged.struct_, paged.type, held, c)) {
       need(held.p != Py_None, "paged_struct() of the cache returned None");
       return;
@@ -460,12 +473,24 @@ struct Pages {
     c.table = static_cast<int32_t *>(ptr_attr(cache, names.table));
     c.seq_len = static_cast<int32_t *>(ptr_attr(cache, names.seq_len));
   }
+  static int bits_of(PyObject *cache) {
+    Held v(PyObject_GetAttr(cache, names.bits));
+    if (!v.p) {  // (a cache that describes itself may know of no others)
+      if (!PyErr_ExceptionMatches(PyExc_AttributeError)) throw Failed();
+      PyErr_Clear();
+      return 2;
+    }
+    const long bits = integer(v.p);
+    need(bits == 2 || bits == 4, "codes have 2 or 4 bits");
+    return (int)bits;
+  }
   // where the pools lie; the two tensors that the caller writes may have been put there by the caller
   void on(PyObject *cache, Here &here) const {
     Held k(PyObject_GetAttr(cache, names.k_codes));
     if (!k.p) throw Failed();
     here(tensor(k.p));
     if (held.p) return;
+    need(bits == 2 || tensor(k.p).numel() == (int64_t)c.n_pages * c.Hkv * c.page_rows * 16, "k_codes is no pool of 4-bit codes");
     Held t(PyObject_GetAttr(cache, names.table)), s(PyObject_GetAttr(cache, names.seq_len));
     if (!t.p || !s.p) throw Failed();
     const at::Tensor &table = tensor(t.p), &len = tensor(s.p);
@@ -506,10 +531,60 @@ PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
       void *const stream = here.stream();
       const void *const k_at = k.data_ptr(), *const v_at = v.data_ptr();
       Py_BEGIN_ALLOW_THREADS
-      status = akvq_paged_append(&pages.c, &chunk, k_at, ks, v_at, vs, clip, flags, stream);
+      status = (pages.bits == 4 ? akvq_paged_nibble_append : akvq_paged_append)(&pages.c, &chunk, k_at, ks, v_at, vs, clip, flags, stream);
       Py_END_ALLOW_THREADS
     }
     return PyLong_FromLong(status);
+  } catch (const Failed &) {
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
+// paged_append_rotary(cache, rotary, pos, q, k, v, row_start, max_rows, clip, q_out, k_out, flags) -> (status, (q_out, k_out))
+PyObject *paged_append_rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 12) {
+    PyErr_SetString(PyExc_TypeError, "paged_append_rotary takes 12 arguments");
+    return nullptr;
+  }
+  try {
+    const Pages pages(a[0]);
+    const akvq_rotary rotary = axes_of<akvq_rotary>(a[1]);
+    const at::Tensor &pos = tensor(a[2]), &v = tensor(a[5]), &row_start = tensor(a[6]);
+    Turned q, k;
+    need(tensor(a[4]).dim() == 3, "k", " has to be fp16 [rows, heads, 128]");
+    const int64_t rows = tensor(a[4]).size(0);
+    k.take(a[4], a[10], "k", "k_out", rows, pages.c.Hkv);
+    if (a[3] == Py_None) need(a[9] == Py_None, "q_out without q");
+    else q.take(a[3], a[9], "q", "q_out", rows, -1);
+    const int64_t vs = packed(v, "v", rows, pages.c.Hkv), pos_stride = positions(pos, rows, rotary.n_axes);
+    const akvq_chunk chunk = chunk_of(pages, row_start, rows, a[7]);
+    const float clip = (float)number(a[8]);
+    const uint32_t flags = flags_of(a[11]);
+    Here here;
+    here(pos);
+    here(tensor(a[4]));
+    for (const at::Tensor *t : {static_cast<const at::Tensor *>(&k.out), &v, &row_start}) here(*t);
+    if (a[3] != Py_None) {
+      here(tensor(a[3]));
+      here(q.out);
+    }
+    pages.on(a[0], here);
+    int status = 0;
+    if (rows > 0) {
+      void *const stream = here.stream();
+      const void *const v_at = v.data_ptr(), *const at_pos = pos.data_ptr();
+      Py_BEGIN_ALLOW_THREADS
+      status = akvq_paged_append_rotary(&pages.c, pages.bits, &chunk, &rotary, static_cast<const int32_t *>(at_pos), pos_stride, q.in, q.stride,
+                                        q.heads, k.in, k.stride, v_at, vs, q.out_at, q.out_stride, k.out_at, k.out_stride, clip, flags, stream);
+      Py_END_ALLOW_THREADS
+      if (a[9] != Py_None) written(q.out);
+      if (a[10] != Py_None) written(k.out);
+    }
+    Held q_out(q.result(a[3], a[9])), k_out(k.result(a[4], a[10]));
+    if (!q_out.p || !k_out.p) return nullptr;
+    return Py_BuildValue("i(OO)", status, q_out.p, k_out.p);
   } catch (const Failed &) {
     return nullptr;
   }
@@ -544,16 +619,17 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *const lse_at = lse.defined() ? lse.data_ptr() : nullptr;
     int status = 0;
     if (rows > 0) {
+      const bool four = pages.bits == 4;
       const int n_split = asked > 0 ? (int)std::min<long>(asked, INT32_MAX)
-                                    : akvq_paged_default_splits(&pages.c, Hq, std::min(chunk.max_rows, chunk.n_rows));
+                                    : (four ? akvq_paged_nibble_default_splits : akvq_paged_default_splits)(&pages.c, Hq, std::min(chunk.max_rows, chunk.n_rows));
       const size_t bytes = n_split <= 1024 ? akvq_paged_workspace_bytes(chunk.n_rows, Hq, n_split) : 0;  // (more is refused by the call)
       at::Tensor ws;  // of its own for every call: calls on two streams, or two captured graphs, share none
       if (bytes) ws = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte).requires_grad(false));
       void *const stream = here.stream(), *const ws_at = bytes ? ws.data_ptr() : nullptr, *const out_at = out.data_ptr();
       const void *const q_at = q.data_ptr(), *const k_at = k.data_ptr(), *const v_at = v.data_ptr();
       Py_BEGIN_ALLOW_THREADS
-      status = akvq_paged_attention(&pages.c, &chunk, q_at, qs, Hq, k_at, ks, v_at, vs, sm_scale, out_at, os,
-                                    static_cast<float *>(lse_at), n_split, ws_at, bytes, flags, stream);
+      status = (four ? akvq_paged_nibble_attention : akvq_paged_attention)(&pages.c, &chunk, q_at, qs, Hq, k_at, ks, v_at, vs, sm_scale, out_at, os,
+                                                                     static_cast<float *>(lse_at), n_split, ws_at, bytes, flags, stream);
       Py_END_ALLOW_THREADS
       if (a[9] != Py_None) written(out);
       if (lse.defined()) written(lse);
@@ -592,6 +668,8 @@ PyMethodDef methods[] = {
     {"plain_paged", plain_paged, METH_VARARGS, nullptr},
     {"rope_axes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rope_axes)), METH_FASTCALL, nullptr},
     {"rope_axes_table", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rope_axes_table)), METH_FASTCALL, nullptr},
+    {"rotary_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotary_rows)), METH_FASTCALL, nullptr},
+    {"paged_append_rotary", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append_rotary)), METH_FASTCALL, nullptr},
     {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
     {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attention)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
@@ -608,7 +686,7 @@ PyMODINIT_FUNC PyInit__akvq_torch(void) {
       {&names.v_win, "v_win"}, {&names.workspace, "workspace"}, {&names.decode, "decode"},
       {&names.struct_, "struct"}, {&names.window_struct, "window_struct"},
       {&names.page_rows, "page_rows"}, {&names.n_pages, "n_pages"}, {&names.max_pages, "max_pages"}, {&names.max_len, "max_len"},
-      {&names.table, "table"}, {&names.seq_len, "seq_len"}, {&names.paged_struct, "paged_struct"}};
+      {&names.table, "table"}, {&names.seq_len, "seq_len"}, {&names.paged_struct, "paged_struct"}, {&names.bits, "bits"}};
   for (auto &t : table)
     if ((*t.slot = PyUnicode_InternFromString(t.text)) == nullptr) return nullptr;
   return PyModule_Create(&module);
