@@ -281,13 +281,19 @@ struct BlockMeta {
 template <int NG>
 struct MetaWords { uint32_t w[NG]; };
 
-template <int NG>
+// a load with the non-temporal hint, or without
+template <bool ONCE, typename T>
+__device__ __forceinline__ T read(const T *p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(p);
+  return *p;
+}
+template <int NG, bool ONCE = false>
 __device__ __forceinline__ MetaWords<NG> load_meta(const uint32_t *at) {
   if constexpr (NG == 2) {
-    const u32x2 w = *reinterpret_cast<const u32x2 *>(at);
+    const u32x2 w = read<ONCE>(reinterpret_cast<const u32x2 *>(at));
     return {{w[0], w[1]}};
   } else {
-    return {{*at}};
+    return {{read<ONCE>(at)}};
   }
 }
 // Scales of 0, which only rows have that were never written, count as the smallest that binary16 holds: their reciprocal is needed.
@@ -418,8 +424,11 @@ struct PagedShared<G, 32, false, BITS> {
   float m[kFewWaves][32], l[kFewWaves][32];
 };
 
-template <int G, int W, bool MANY, int BITS>
+// EIGHT: no workgroup has more than eight rows (of a tile of 16): the two columns of each also share the digits of its query.
+template <int G, int W, bool MANY, int BITS, bool EIGHT = false>
 __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(BITS == 4 && G == 64) ? 3 : 2) void paged_attention_kernel(PagedAttentionArgs a) {
+  static_assert(BITS == 2 || kDigits == 4);
+  static_assert(!EIGHT || (W == 16 && BITS == 4));
   typedef Tile<W> T;
   typedef typename T::Acc Acc;
   constexpr int NG = kD / G, NW = MANY ? kManyWaves : kFewWaves, WK = MANY ? 1 : NW, kWide = W == 32;
@@ -435,14 +444,39 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
   // Unequal sequences, where a CU gets few workgroups: which ones decides.  Where it holds one (many rows), the longest begin first; where it
   // holds two or three, the first on every CU go from long to short, the second from short to long.
   ChunkSpan s;
-  if (MANY ? c.B <= kWave : c.B <= kWave && gridDim.x > kCus && gridDim.y * gridDim.z == 1) {
+  const bool ordered = MANY ? c.B <= kWave : c.B <= kWave && gridDim.x > kCus && gridDim.y * gridDim.z == 1;
+  // Few rows: the pages' numbers where two loads hold them all (lane l: of pages window + l and window + 64 + l), and the beginning of the list of
+  // 16-bit rows: asked for with the lengths where these decide nothing
+  const bool short_table = c.max_pages <= 2 * kWave;
+  [[maybe_unused]] int window = 0, pages = 0, next_pages = 0;
+  int entry = 0, listed = 0;
+  auto ask_table = [&](int from) { return c.table[(size_t)b * c.max_pages + min(from + lane, c.max_pages - 1)]; };
+  auto ask_lists = [&] {
+    if (!MANY && short_table) {
+      pages = ask_table(0);
+      next_pages = ask_table(kWave);
+    }
+    const size_t unit = (size_t)b * c.Hkv + head;
+    entry = c.sal_idx[unit * c.S_cap + lane];  // (S_cap >= 64)
+    listed = c.sal_cnt[unit];
+  };
+  constexpr bool kEarlyLists = !MANY && BITS == 4;
+  if (kEarlyLists && !ordered) ask_lists();
+  if (ordered) {
     const int me = min(lane, c.B - 1);
     const ChunkSpan mine = chunk_span(c.seq_len[me], c.row_start[me], c.row_start[me + 1], c);
     const int tiles = lane >= c.B ? 0 : MANY ? (mine.rows * R + kRows - 1) / kRows : 1, keys = mine.len + mine.rows;
     int begin = 0;  // of this lane's sequence in that order, in tiles
-    for (int x = 0; x < c.B; ++x) {
-      const int other = __builtin_amdgcn_readlane(keys, x);
-      if (other > keys || (other == keys && x < lane)) begin += __builtin_amdgcn_readlane(tiles, x);
+    if constexpr (kEarlyLists) {  // one tile each: how many are longer, by keys that no two lanes share (lengths past 2^24 count alike)
+      const int mine_key = lane < c.B ? min(keys, (1 << 24) - 1) * kWave + (kWave - 1 - lane) : -1;
+      for (int x = 0; x < c.B; x += 8)
+#pragma unroll
+        for (int y = 0; y < 8; ++y) begin += __builtin_amdgcn_readlane(mine_key, x + y) > mine_key;
+    } else {
+      for (int x = 0; x < c.B; ++x) {
+        const int other = __builtin_amdgcn_readlane(keys, x);
+        if (other > keys || (other == keys && x < lane)) begin += __builtin_amdgcn_readlane(tiles, x);
+      }
     }
     int at = blockIdx.y * c.B + b;
     if constexpr (!MANY) {
@@ -469,7 +503,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
   // apart, so that their roundings differ and half as much is left in the sum of both: 1.1e-4 of a weight, 2.1e-4 of one column.  Outputs are off by
   // 2.4e-4 of their norm in place of 2.9e-4 (2.1e-4 is their own rounding), for 0.25 us of a call over 640 rows and 1 % of long ones.  (The
   // second column for what the first one's rounding drops would leave 2.1e-4, and takes 6 to 17 %.)
-  const bool twice = W == 16 && rows - wg_row <= 8;
+  const bool twice = EIGHT || (W == 16 && rows - wg_row <= 8);
   auto apart = [&] { return twice && (lane & 8) ? kApart : 0.0f; };
   const int my_row = min(row0 + (twice ? col & 7 : col), rows - 1), my_token = my_row / R;
   const float sm2 = a.sm_scale * kLog2e;
@@ -480,25 +514,15 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
 #pragma unroll
     for (int k = 0; k < NC; ++k) raw[k] = *reinterpret_cast<const u32x4 *>(q_at + kD / NC * k);
   };
-  // Few rows: what needs nothing but the sequence is asked for in front of the search for its 16-bit rows: the query, and the pages' numbers where
-  // two loads hold them all (lane l: of pages window + l and window + 64 + l)
+  // Few rows: what needs nothing but the sequence is asked for in front of the search for its 16-bit rows: the query, too
   const int32_t *table = c.table + (size_t)b * c.max_pages;
-  auto ask_table = [&](int from) { return table[min(from + lane, c.max_pages - 1)]; };
-  const bool short_table = c.max_pages <= 2 * kWave;
-  [[maybe_unused]] int window = 0, pages = 0, next_pages = 0;
+  if (!kEarlyLists || ordered) ask_lists();
   [[maybe_unused]] u32x4 early_query[NC];
-  if constexpr (!MANY) {
-    if (short_table) {
-      pages = ask_table(0);
-      next_pages = ask_table(kWave);
-    }
-    load_query(early_query);
-  }
+  if constexpr (!MANY) load_query(early_query);
 
   // ---- the keys of this workgroup: blocks of 32 code rows, of 32 overlay slots, of 32 chunk rows, dealt to the splits as one list
   const int32_t *sidx = c.sal_idx + (size_t)unit * c.S_cap;
-  const int entry = sidx[lane];                                 // (S_cap >= 64: asked for together with the count)
-  int wide = min(max(c.sal_cnt[unit], 0), c.S_cap);             // overlay slots of cached rows (the list may be final for new rows, too)
+  int wide = min(max(listed, 0), c.S_cap);                      // overlay slots of cached rows (the list may be final for new rows, too)
   if (wide <= kWave) {
     wide = __popcll(__ballot(lane < wide && entry < s.len));
   } else {
@@ -529,8 +553,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
   // per column: the reference that weights are relative to, from which excess over it it is raised (before the first score: any), and
   // this lane's share of the sum
   float m = 0.0f, limit = 0.5f * kNoScore, l = 0.0f;
-  // the rotated query, times sm_scale * log2(e): products with it are base-2 logits
-  auto rotated = [&](const u32x4 (&raw)[NC], float (&x)[8 * NC]) {
+  // the rotated query without its factor, which is returned; and times it, sm_scale * log2(e) in it: products with that are base-2 logits
+  auto turned = [&](const u32x4 (&raw)[NC], float (&x)[8 * NC]) {
     float f = sm2;
     if (!a.q_rotated) {
       rotate_query_columns(raw, x, lane);
@@ -544,6 +568,10 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
           x[8 * k + 2 * w + 1] = half_bits_to_float(raw[k][w] >> 16);
         }
     }
+    return f;
+  };
+  auto rotated = [&](const u32x4 (&raw)[NC], float (&x)[8 * NC]) {
+    const float f = turned(raw, x);
 #pragma unroll
     for (int e = 0; e < 8 * NC; ++e) x[e] *= f;
   };
@@ -620,13 +648,14 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
     // Four bits, W = 32: all words of chunks h and 2 + h in the block's half p; W = 16: of a chunk in both halves.  (Halves are rows of keys and
     // every other channel block of values.)
     typedef RowWords<BITS> Words;
+    constexpr bool kOnce = EIGHT;  // one workgroup reads them: with the non-temporal hint
     auto load_codes = [&](const uint32_t *pool, const Where &at) {
       const uint32_t *blk = pool + at.row * (4 * BITS);
       Words words;
       if constexpr (BITS == 4) {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
-          words.w[x] = *reinterpret_cast<const u32x4 *>(blk + (kWide ? 256 * p + (32 * x + 16 * g_lane + n) * 4 : 256 * x + 4 * lane));
+          words.w[x] = read<kOnce>(reinterpret_cast<const u32x4 *>(blk + (kWide ? 256 * p + (32 * x + 16 * g_lane + n) * 4 : 256 * x + 4 * lane)));
       } else if constexpr (kWide) {
         const u32x2 x = *reinterpret_cast<const u32x2 *>(blk + (16 * g_lane + n) * 4 + 2 * p), y = *reinterpret_cast<const u32x2 *>(blk + (32 + 16 * g_lane + n) * 4 + 2 * p);
         words.w[0] = (u32x4){x[0], x[1], y[0], y[1]};
@@ -663,8 +692,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
     constexpr bool kOneValue = kWide && BITS == 4 && NG == 2;  // registers for one block's values: asked for a block ahead
     auto ask_meta = [&](const Pair &p) {
       const size_t row = ((lane < 32 ? p.at[0].row : p.at[1].row) + (lane & 31)) * NG;
-      few_kw = load_meta<NG>(c.k_meta + row);
-      few_vw = load_meta<NG>(c.v_meta + row);
+      few_kw = load_meta<NG, kOnce>(c.k_meta + row);
+      few_vw = load_meta<NG, kOnce>(c.v_meta + row);
     };
     auto row_there = [&](int blk, const Pair &p) { return (blk + (lane >> 5)) * 32 + (lane & 31) < (lane < 32 ? p.at[0].limit : p.at[1].limit); };
     Pair now = {}, next = {};
@@ -683,37 +712,48 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
       }
       next = locate(first + 2);
     }
-    u32x6 digits[NP][kDigits];
-    uint32_t unit_exp;
+    // EIGHT: product P takes digit P of a row in its first column and digit 2 + P in its second
+    constexpr int ND = EIGHT ? kDigits / 2 : kDigits;
+    u32x6 digits[NP][ND];
+    // exponents of the digits, a byte a product.  8-bit rows of both groups meet in one product (W = 16): its other group's lanes get 2^-127
+    constexpr int NU = BITS == 4 && !kWide ? NG : 1;
+    uint32_t unit_exp[NU];
     u32x4 start[NG];  // column operands of the first product: terms of the query's sum, of minus the reference, ones
     auto start_slots = [&](float v, uint32_t ones) {
       const Terms x = split_terms(v);
       return (u32x4){upper_halves(x.a, x.b), upper_halves(x.c, x.a), upper_halves(x.b, g_lane == 1 ? x.a : x.c), ones};
     };
     {
-      float x[8 * NC], mx = 0.0f;
+      float x[8 * NC], mx = 0.0f, factor = 1.0f;
+      auto prepare = [&](const u32x4 (&raw)[NC]) {
+        if constexpr (BITS == 4) factor = turned(raw, x);
+        else rotated(raw, x);
+      };
       if constexpr (MANY) {
         u32x4 raw[NC];
         load_query(raw);
-        rotated(raw, x);
+        prepare(raw);
       } else {
-        rotated(early_query, x);
+        prepare(early_query);
       }
 #pragma unroll
       for (int e = 0; e < 8 * NC; ++e) mx = fmaxf(mx, fabsf(x[e]));
       mx = T::column_max(mx);
+      if constexpr (BITS == 4) mx *= fabsf(factor);
       // integers of up to 5 kDigits - 1 bits and a sign in units of a power of two U, |x| < 2^(5 kDigits - 1) U
-      const uint32_t e_biased = min(max(__float_as_uint(mx) >> 23, 20u), 250u);  // mx < 2^(e_biased - 126)
+      const uint32_t e_biased = min(max(__float_as_uint(mx) >> 23, BITS == 4 ? 64u : 20u), 250u);  // mx < 2^(e_biased - 126)
       const float unit_inv = __uint_as_float((252u + 5u * kDigits - e_biased) << 23), u = 1.0f / unit_inv;
       float sum[2] = {0.0f, 0.0f};
       // digit k of n is the signed five-bit field k of ((n + b) ^ b), b = 16 in every lower digit
       constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer in the low bits
       constexpr int kHalf = kDigits == 4 ? 16 * (1 + 32 + 1024) : 16 * (1 + 32);
       int v[8 * NC];
+      // (4 bits: the factor and the unit at once, queries below 2^-62 in units of 2^-82; no unit that is infinite meets a query of zeros)
+      const float to_unit = BITS == 4 ? fminf(fmaxf(factor * unit_inv, -3.0e38f), 3.0e38f) : unit_inv;
 #pragma unroll
       for (int e = 0; e < 8 * NC; ++e) {
-        const float t = __builtin_fmaf(x[e], unit_inv, kMagic);
-        sum[e / (4 * NC)] += t - kMagic;  // (the upper half of a lane's channels is the second group)
+        const float t = __builtin_fmaf(x[e], to_unit, kMagic);
+        if constexpr (BITS == 2) sum[e / (4 * NC)] += t - kMagic;  // (the upper half of a lane's channels is the second group)
         v[e] = (__float_as_int(t) + (kHalf - 0x4B400000)) ^ kHalf;
       }
       auto make_digit = [&](int pr, int shift, int bits) {
@@ -751,25 +791,52 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
 #pragma unroll
         for (int pr = 0; pr < NP; ++pr)
 #pragma unroll
-          for (int d = 0; d < kDigits; ++d)
+          for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int i = 0; i < 6; ++i) {
               // 8-bit rows: the product's inner slots 32L .. 32L + 31, which 6-bit digits of lane group L hold, lie in two lane groups of the rows,
               // sixteen in each: the lower or the upper half of their slots
               const int L = lane / W, from = kWide ? col + 32 * (i / 3) : col + 16 * (2 * (L & 1) + i / 3), word = i % 3 + 3 * (kWide ? L : L >> 1);
-              digits[pr][d][i] = BITS == 2 ? sh.digits[pr][d][i][lane] : sh.digits[pr][d][word][from];
+              digits[pr][d][i] = BITS == 2 ? sh.digits[pr][d][i][lane] : sh.digits[pr][EIGHT ? d + 2 * (col >> 3) : d][word][from];
             }
         lds_barrier();  // (what comes last lies where the digits were)
       }
-      sum[0] *= u;
-      sum[1] *= u;
-      const float s0 = T::column_sum(NG == 2 ? sum[0] : sum[0] + sum[1]);
-      start[0] = start_slots(g_lane == 0 ? s0 : g_lane == 1 ? apart() : 0.0f, g_lane == 0 ? 0x3F803F80u : g_lane == 1 ? 0x00003F80u : 0u);
-      if constexpr (NG == 2) {
-        const float s1 = T::column_sum(sum[1]);
-        start[1] = start_slots(g_lane == 0 ? s1 : 0.0f, 0u);
+      unit_exp[0] = (e_biased + 6u - 5u * kDigits) * 0x01010101u + 0x0F0A0500u;  // a byte a digit: each 32 times the one below
+      if (EIGHT && col >= 8) unit_exp[0] >>= 16;
+      if constexpr (NU == 2) {
+        unit_exp[1] = g_lane >= 2 ? unit_exp[0] : 0u;
+        unit_exp[0] = g_lane < 2 ? unit_exp[0] : 0u;
       }
-      unit_exp = (e_biased + 6u - 5u * kDigits) * 0x01010101u + 0x0F0A0500u;  // a byte a digit: each 32 times the one below
+      if constexpr (BITS == 4) {  // the sums of a group's channels: products with rows of ones, 2^-9 as 8-bit floats, 1 / 8 as 6-bit ones
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          Acc acc = T::zero();
+#pragma unroll
+          for (int pr = 0; pr < NP; ++pr) {
+            if (NG == 2 && NP == 2 && pr != g) continue;
+            auto add = [&](auto ones) {
+              const uint32_t scale = unit_exp[NU == 2 ? g : 0];
+              acc = T::template codes<0>(ones, digits[pr][0], scale, acc);
+              acc = T::template codes<1>(ones, digits[pr][1], scale, acc);
+              if constexpr (!EIGHT) {
+                acc = T::template codes<2>(ones, digits[pr][2], scale, acc);
+                acc = T::template codes<3>(ones, digits[pr][kDigits - 1], scale, acc);
+              }
+            };
+            constexpr uint32_t kOne = 0x01010101u;
+            if constexpr (MANY) add((u32x6){0x41041041u, 0x10410410u, 0x04104104u, 0x41041041u, 0x10410410u, 0x04104104u});
+            else add((u32x8){kOne, kOne, kOne, kOne, kOne, kOne, kOne, kOne});
+          }
+          sum[g] = EIGHT ? acc[0] + other_eight(acc[0]) : acc[0];
+        }
+      } else {
+        sum[0] = T::column_sum(NG == 2 ? sum[0] * u : sum[0] * u + sum[1] * u);
+        if constexpr (NG == 2) sum[1] = T::column_sum(sum[1] * u);
+      }
+      // (EIGHT: in the first column, whose products the second one's are added to)
+      const bool none = EIGHT && col >= 8;
+      start[0] = start_slots(none ? 0.0f : g_lane == 0 ? sum[0] : g_lane == 1 && !EIGHT ? apart() : 0.0f, none ? 0u : g_lane == 0 ? 0x3F803F80u : g_lane == 1 ? 0x00003F80u : 0u);
+      if constexpr (NG == 2) start[1] = start_slots(none || g_lane != 0 ? 0.0f : sum[1], 0u);
     }
     // scores of a block; codes(product): the row operand (W = 16: of the half that is being formed)
     auto scores = [&](const auto &bm, float (&y)[NY], auto &&codes) {
@@ -786,10 +853,19 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
         for (int pr = 0; pr < (kWide ? 2 : NG); ++pr) {
           const int g = NG == 2 ? pr : 0, of = kWide ? pr : 0;
           const auto rows = codes(pr, half);
-          acc[g] = T::template codes<0>(rows, digits[of][0], unit_exp, acc[g]);
-          acc[g] = T::template codes<1>(rows, digits[of][1], unit_exp, acc[g]);
-          acc[g] = T::template codes<2>(rows, digits[of][2], unit_exp, acc[g]);
-          if constexpr (kDigits == 4) acc[g] = T::template codes<kDigits - 1>(rows, digits[of][kDigits - 1], unit_exp, acc[g]);
+          const uint32_t scale = unit_exp[NU == 2 ? pr : 0];
+          acc[g] = T::template codes<0>(rows, digits[of][0], scale, acc[g]);
+          acc[g] = T::template codes<1>(rows, digits[of][1], scale, acc[g]);
+          if constexpr (!EIGHT) {
+            acc[g] = T::template codes<2>(rows, digits[of][2], scale, acc[g]);
+            if constexpr (kDigits == 4) acc[g] = T::template codes<kDigits - 1>(rows, digits[of][kDigits - 1], scale, acc[g]);
+          }
+        }
+        if constexpr (EIGHT) {
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[g][i] += other_eight(acc[g][i]);
         }
 #pragma unroll
         for (int x = 0; x < (kWide ? 4 : 1); ++x) {
@@ -799,7 +875,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
             const f32x4 scale = *reinterpret_cast<const f32x4 *>(&bm.k_scale[g][T::row(at, g_lane)]);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              y[4 * at + i] = g == 0 ? scale[i] * acc[0][4 * x + i] : __builtin_fmaf(scale[i], acc[g][4 * x + i], y[4 * at + i]);
+              y[4 * at + i] = g == 0 ? EIGHT ? __builtin_fmaf(scale[i], acc[0][4 * x + i], apart()) : scale[i] * acc[0][4 * x + i]
+                                     : __builtin_fmaf(scale[i], acc[g][4 * x + i], y[4 * at + i]);
           }
         }
       }
@@ -808,7 +885,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
       raise([&](float alpha) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) acc_z[g] *= alpha;
-        if (g_lane == 1) start[0] = start_slots(apart() - m, 0x00003F80u);
+        if (g_lane == 1 && !(EIGHT && col >= 8)) start[0] = start_slots(EIGHT ? -m : apart() - m, 0x00003F80u);
       }, y...);
     };
     // weights of a block's scores, and their sum
@@ -1069,10 +1146,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
             return (u32x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
           } else if constexpr (BITS == 4) {
             const u32x4 w = few_k[x].w[half];
-            const u32x2 none = {0u, 0u}, a = nibbles(w[0]), b = nibbles(w[1]), c = nibbles(w[2]), d = nibbles(w[3]);
-            const bool lower = NG == 1 || pr == 0, upper = NG == 1 || pr == 1;
-            const u32x2 a0 = lower ? a : none, b0 = lower ? b : none, c0 = upper ? c : none, d0 = upper ? d : none;
-            return (u32x8){a0[0], a0[1], b0[0], b0[1], c0[0], c0[1], d0[0], d0[1]};
+            const u32x2 a = nibbles(w[0]), b = nibbles(w[1]), c = nibbles(w[2]), d = nibbles(w[3]);
+            return (u32x8){a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
           } else if constexpr (kWide) {
             const u32x2 lo = ex4(few_k[x].w[0][pr]), hi = ex4(few_k[x].w[0][2 + pr]);
             return (u32x4){lo[0], lo[1], hi[0], hi[1]};
@@ -1085,12 +1160,18 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
       };
       bool far = false;
       if (first < code_end) far = decode_pair<NG, BITS>(few_kw, few_vw, row_there(first, now), bms[0], lane);
-      ask_meta(next);
+      if (!EIGHT || first + 2 < code_end) ask_meta(next);
       wave_lds_sync();
       for (int blk = first, turn = 0; blk < code_end; blk += 2, turn ^= 1) {
-        const bool next_far = decode_pair<NG, BITS>(few_kw, few_vw, row_there(blk + 2, next), bms[turn ^ 1], lane);
-        const Pair after = locate(blk + 4);
-        ask_meta(after);
+        bool next_far = false;
+        Pair after = next;
+        // (up to eight rows: nothing is asked or waited for that is not used)
+        const bool more = !EIGHT || blk + 2 < code_end;
+        if (more) {
+          next_far = decode_pair<NG, BITS>(few_kw, few_vw, row_there(blk + 2, next), bms[turn ^ 1], lane);
+          after = locate(blk + 4);
+          if (!EIGHT || blk + 4 < code_end) ask_meta(after);
+        }
         const BlockMeta<NG> (&bm)[2] = bms[turn];
         if constexpr (kWide) {
 #pragma unroll
@@ -1098,26 +1179,28 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
             if (x == 1 && blk + 1 >= code_end) break;
             float y[NY];
             scores(bm[x], y, codes_of(x));
-            few_k[x] = load_codes(c.k_codes, next.at[x]);
+            if (more) few_k[x] = load_codes(c.k_codes, next.at[x]);
             raise_codes(y);
             weights(bm[x], y);
             values(few_v[kOneValue ? 0 : x], bm[x], far, y);
             if constexpr (kOneValue) few_v[0] = load_codes(c.v_codes, x == 0 ? now.at[1] : next.at[0]);
-            else few_v[x] = load_codes(c.v_codes, next.at[x]);
+            else if (more) few_v[x] = load_codes(c.v_codes, next.at[x]);
           }
         } else {  // both at once: what one waits for the other covers
           float y0[NY], y1[NY];
           scores(bm[0], y0, codes_of(0));
           scores(bm[1], y1, codes_of(1));
+          if (more)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) few_k[x] = load_codes(c.k_codes, next.at[x]);
+            for (int x = 0; x < 2; ++x) few_k[x] = load_codes(c.k_codes, next.at[x]);
           raise_codes(y0, y1);
           weights(bm[0], y0);
           weights(bm[1], y1);
           values(few_v[0], bm[0], far, y0);
           values(few_v[1], bm[1], far, y1);
+          if (more)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) few_v[x] = load_codes(c.v_codes, next.at[x]);
+            for (int x = 0; x < 2; ++x) few_v[x] = load_codes(c.v_codes, next.at[x]);
         }
         if constexpr (kOneValue) now = next;
         next = after;
@@ -1184,6 +1267,9 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
 
   // ================= 16-bit rows of the cache =================
   if (wide_begin < wide_end) {
+    const uint16_t *ks = c.k_sal + (size_t)unit * c.S_cap * kD, *vs = c.v_sal + (size_t)unit * c.S_cap * kD;
+    auto key_at = [&](int blk, int half, int k) { return reinterpret_cast<const u32x4 *>(ks + (size_t)(blk * 32 + 16 * half + col) * kD + kD / NC * k + 8 * g_lane); };
+    auto value_at = [&](int blk, int nb, int g) { return reinterpret_cast<const u32x4 *>(vs + (size_t)blk * 4096 + nb * 512 + 8 * (16 * g + n)); };
     {
       u32x4 raw[NC];
       float x[8 * NC];
@@ -1191,7 +1277,6 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
       rotated(raw, x);
       split_query(x);
     }
-    const uint16_t *ks = c.k_sal + (size_t)unit * c.S_cap * kD, *vs = c.v_sal + (size_t)unit * c.S_cap * kD;
     // one block of 32 slots; value(nb, g): the 16 bytes of the tile for channels 16nb + n, rows 4g + i and 16 + 4g + i
     auto wide_block = [&](int blk, auto &&key, auto &&value) {
       float y[NY];
@@ -1240,8 +1325,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
              });
     } else {
       for (int blk = wide_begin; blk < wide_end; ++blk)
-        wide_block(blk, [&](int half, int k) { return *reinterpret_cast<const u32x4 *>(ks + (size_t)(blk * 32 + 16 * half + col) * kD + kD / NC * k + 8 * g_lane); },
-                   [&](int nb, int g) { return *reinterpret_cast<const u32x4 *>(vs + (size_t)blk * 4096 + nb * 512 + 8 * (16 * g + n)); });
+        wide_block(blk, [&](int half, int k) { return *key_at(blk, half, k); }, [&](int nb, int g) { return *value_at(blk, nb, g); });
     }
   }
   // The cached rows' share is rotated back (H is its own inverse), and the chunk's rows join it.  Their weights are relative to the
@@ -1537,7 +1621,8 @@ void launch_variant(const PagedAttentionArgs &a, int rows, hipStream_t stream) {
   constexpr int kFew = 64 * kFewWaves, kMany = 64 * kManyWaves;
   static_assert(kPagedManyRows == 32 * kManyWaves);
   const long per = paged_tile_rows(units, a.c.max_rows, a.Hq / a.c.Hkv, a.c.max_len);
-  if (per == 16) paged_attention_kernel<G, 16, false, BITS><<<grid(16), kFew, 0, stream>>>(a);
+  if (BITS == 4 && per == 16 && rows <= 8) paged_attention_kernel<G, 16, false, BITS, BITS == 4><<<grid(16), kFew, 0, stream>>>(a);
+  else if (per == 16) paged_attention_kernel<G, 16, false, BITS><<<grid(16), kFew, 0, stream>>>(a);
   else if (per == 32) paged_attention_kernel<G, 32, false, BITS><<<grid(32), kFew, 0, stream>>>(a);
   else paged_attention_kernel<G, 32, true, BITS><<<grid(kPagedManyRows), kMany, 0, stream>>>(a);
 }
