@@ -83,6 +83,12 @@ int append_args(const akvq_paged *c, const akvq_chunk *rows, const void *k, int6
   return AKVQ_OK;
 }
 
+int default_splits(const akvq_paged *c, int Hq, int max_rows, int bits) {
+  if (check_paged_shape(c) != AKVQ_OK || Hq <= 0 || Hq % c->Hkv != 0 || max_rows <= 0) return 1;
+  const int64_t cap = (int64_t)c->max_pages * c->page_rows;
+  return akvq::paged_splits((long)c->B * c->Hkv, max_rows, Hq / c->Hkv, (long)(c->max_len < cap ? c->max_len : cap), {bits, c->G});
+}
+
 // Arguments of attention over pages; default_splits: the library's choice for the caller's bound.  a.c.max_rows is 0 where there is nothing to do.
 template <typename Splits>
 int attention_args(const akvq_paged *c, const akvq_chunk *rows, const void *q, int64_t q_stride, int Hq, const void *k, int64_t k_stride,

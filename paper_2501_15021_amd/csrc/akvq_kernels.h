@@ -432,7 +432,11 @@ constexpr int kPagedManyRows = 256;  // of a workgroup that has many; its number
 // 32 units, 256 workgroups 21.1, 512 18.1, 768 20.1; of 256 units, 256 106, 512 79, 768 72; 32 rows (R = 4) over 32768 of 32 units, in tiles of
 // 32, 256 40.4, 512 37.0; of 256 units over 4096, 256 38.5, 512 42.7, over 8192 70 and 64; one row over 640 of 32 units, 2 splits 10.8, 5
 // splits 9.5.
-inline long paged_tile_splits(long per, long units, long tokens, long R, long len) {
+// Codes of 4 bits: with one group a row three workgroups of 16 rows run on a CU, and rounds of them even out what memory gives each: one row
+// over 16384 rows of 512 units, 512 workgroups 219, 1536 190, 2048 188; of 256 units over up to 16384, 768 81.5, 1536 78.6; with two groups two
+// run: over 32768 of 128 units, 512 116, 768 128, 1024 122, over up to 16384, 58, 70 and 63.
+struct PagedKind { int bits = 2, G = 128; };
+inline long paged_tile_splits(long per, long units, long tokens, long R, long len, PagedKind kind = {}) {
   const long blocks = (len + tokens + 31) / 32, tiles = (tokens * R + per - 1) / per;
   long want = 1;
   auto fill = [&](long workgroups, long least) {
@@ -440,7 +444,11 @@ inline long paged_tile_splits(long per, long units, long tokens, long R, long le
     if (n > blocks / least) n = blocks / least;
     if (n > want) want = n;
   };
-  if (per == 16) { fill(256, 4); fill(512, 8); fill(768, 64); }
+  if (per == 16) {
+    fill(256, 4); fill(512, 8);
+    if (kind.bits == 2 || kind.G == 128) fill(768, 64);
+    if (kind.bits == 4 && kind.G == 128) fill(2304, 85);
+  }
   else if (per == 32) { fill(256, 8); fill(512, want == 1 ? 128 : 32); }
   else fill(256, 8);
   return want < 64 ? want : 64;
@@ -448,12 +456,12 @@ inline long paged_tile_splits(long per, long units, long tokens, long R, long le
 // What a call takes in tiles of 32 or 256 rows, in us, by rounds of workgroups (two on a CU, or one): a beginning and end, and for every block
 // of 32 keys what was measured on full CUs.  Up to 11 % off the measurements below for tiles of 32 and 19 % for tiles of 256, the nearest pair 6 % apart
 // and 1 % in the estimate; it is there to compare the two, and is right in all nine.
-inline double paged_tile_cost(long per, long units, long tokens, long R, long len) {
-  const long rows = tokens * R, tiles = (rows + per - 1) / per, splits = paged_tile_splits(per, units, tokens, R, len);
+inline double paged_tile_cost(long per, long units, long tokens, long R, long len, PagedKind kind = {}) {
+  const long rows = tokens * R, tiles = (rows + per - 1) / per, splits = paged_tile_splits(per, units, tokens, R, len, kind);
   const double cached = len / 32.0, own = tokens / 32.0, merge = splits > 1 ? 5.0 : 0.0;
   double rounds = (double)(units * tiles * splits) / (per == 32 ? 512 : 256);
   if (rounds < 1.0) rounds = 1.0;
-  if (per == 32) return rounds * (10.0 + (0.32 * cached + 0.5 * own) / splits) + merge;
+  if (per == 32) return rounds * (10.0 + ((kind.bits == 4 ? 0.38 : 0.32) * cached + 0.5 * own) / splits) + merge;
   return rounds * (18.0 + (0.44 + 0.1 * (rows / 32.0 / tiles)) * (cached + own) / splits) + merge;  // (per wavefront that has rows)
 }
 // How many rows (tokens x heads of a group) a workgroup takes: 16 or 32, which its four wavefronts share, or 256, 32 for each of eight that
@@ -463,15 +471,19 @@ inline double paged_tile_cost(long per, long units, long tokens, long R, long le
 //   tiles of 32 or of 256, the better split of each: 256 units of 96 rows over 4096 85 and 97, of 200 188 and 151; 128 of 128 rows over 8192 95 and
 //     112, of 256 185 and 172; 64 of 256 94 and 102; 4 of 585 tokens (R = 7) over 2048 39 and 54; 4 of 1024 (R = 4) over 32768 320 and 302;
 //     4 of 4096 over 64 71 and 59, 8 of 2048 42 and 48.
-inline long paged_tile_rows(long units, long tokens, long R, long len) {
+// Codes of 4 bits, the same way: 28 rows of 32 units over 16384 (R = 7, G = 64) 36.0 in two tiles of 16 and 33.4 in one of 32, of 128 units 115 and
+// 91; 32 rows of 64 units over 8192 30.0 and 31.6; in tiles of 32 or 256, 256 units of 96 rows over 4096 100 and 121, of 200 221 and 165; 128 of 128
+// rows over 8192 110 and 125, of 256 214 and 191; 64 of 256 112 and 106; 4 of 585 tokens (R = 7, G = 64) over 2048 53 and 60; 8 of 1024 (R = 4)
+// over 32768 744 and 640.
+inline long paged_tile_rows(long units, long tokens, long R, long len, PagedKind kind = {}) {
   const long rows = tokens * R;
-  if (rows <= 16 || (rows <= 32 && units * ((len + 31) / 32) < 1L << 15)) return 16;
+  if (rows <= 16 || (rows <= 32 && units * ((len + 31) / 32) < 1L << (kind.bits == 4 && kind.G == 64 ? 14 : 15))) return 16;
   if (rows <= 64) return 32;
   if (rows > 65535L * 32) return kPagedManyRows;  // (tiles are a grid dimension)
-  return paged_tile_cost(32, units, tokens, R, len) <= paged_tile_cost(kPagedManyRows, units, tokens, R, len) ? 32 : kPagedManyRows;
+  return paged_tile_cost(32, units, tokens, R, len, kind) <= paged_tile_cost(kPagedManyRows, units, tokens, R, len, kind) ? 32 : kPagedManyRows;
 }
-inline int paged_splits(long units, long tokens, long R, long len) {
-  return (int)paged_tile_splits(paged_tile_rows(units, tokens, R, len), units, tokens, R, len);
+inline int paged_splits(long units, long tokens, long R, long len, PagedKind kind = {}) {
+  return (int)paged_tile_splits(paged_tile_rows(units, tokens, R, len, kind), units, tokens, R, len, kind);
 }
 
 // ---- pages of 4-bit codes: the same calls over pools of twice the words (akvq_paged4.hip, akvq_paged4_attention.hip) ----

@@ -1620,7 +1620,7 @@ void launch_variant(const PagedAttentionArgs &a, int rows, hipStream_t stream) {
   auto grid = [&](int per) { return dim3(units, (rows + per - 1) / per, a.n_split); };
   constexpr int kFew = 64 * kFewWaves, kMany = 64 * kManyWaves;
   static_assert(kPagedManyRows == 32 * kManyWaves);
-  const long per = paged_tile_rows(units, a.c.max_rows, a.Hq / a.c.Hkv, a.c.max_len);
+  const long per = paged_tile_rows(units, a.c.max_rows, a.Hq / a.c.Hkv, a.c.max_len, {BITS, G});
   if (BITS == 4 && per == 16 && rows <= 8) paged_attention_kernel<G, 16, false, BITS, BITS == 4><<<grid(16), kFew, 0, stream>>>(a);
   else if (per == 16) paged_attention_kernel<G, 16, false, BITS><<<grid(16), kFew, 0, stream>>>(a);
   else if (per == 32) paged_attention_kernel<G, 32, false, BITS><<<grid(32), kFew, 0, stream>>>(a);

@@ -50,7 +50,7 @@ int akvq_paged_nibble_append(const akvq_paged *c, const akvq_chunk *rows, const 
   return akvq::launch_status(akvq::launch_paged4_append(a, c->G, static_cast<hipStream_t>(stream)));
 }
 
-int akvq_paged_nibble_default_splits(const akvq_paged *c, int Hq, int max_rows) { return akvq_paged_default_splits(c, Hq, max_rows); }
+int akvq_paged_nibble_default_splits(const akvq_paged *c, int Hq, int max_rows) { return default_splits(c, Hq, max_rows, 4); }
 
 int akvq_paged_nibble_attention(const akvq_paged *c, const akvq_chunk *rows, const void *q, int64_t q_stride, int Hq, const void *k,
                           int64_t k_stride, const void *v, int64_t v_stride, float sm_scale, void *out, int64_t out_stride,
