@@ -51,9 +51,9 @@ __device__ __forceinline__ void block_slots(const int32_t *sidx, int cnt, int t0
 // row is not (uniform over the wavefront).
 template <int G, int BITS, int TENSOR>
 __device__ __forceinline__ void append_block(const PagedArgs &c, size_t unit, int t0, size_t row0, const u32x4 (&raw)[2][4], const bool (&valid)[2],
-                                             bool partial_blk, bool rotate, float clip, int *slot_of) {
+                                             bool partial_blk, bool rotate, float clip, int *slot_of, int lane) {
   constexpr int NG = kD / G;
-  const int lane = threadIdx.x & 63, r = lane >> 2, j = lane & 3, ii = r & 3, q = r >> 2;
+  const int r = lane >> 2, j = lane & 3, ii = r & 3, q = r >> 2;
   const size_t blk_word = row0 / kTokBlock * (BITS * kBlockWords / 2);
   const float kappa = rotate ? inv_sqrt128() : 1.0f;
   const float lane_sign = rotate ? quad_sign(j) : 1.0f;  // this lane holds lane_sign * (transformed values)

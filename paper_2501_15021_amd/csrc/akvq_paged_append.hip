@@ -44,7 +44,7 @@ __device__ __forceinline__ void paged_append_body(const PagedAppendArgs &a, int 
     for (int m = 0; m < 4; ++m) raw[h][m] = *reinterpret_cast<const u32x4 *>(row + 32 * m + 8 * j);
   }
   append_block<G, BITS, TENSOR>(c, blockIdx.y, t0, row0, raw, valid, t0 < s.len || t0 + kTokBlock > t_end,
-                                (TENSOR == 0 ? a.rotate_k : a.rotate_v) != 0, a.clip, slot_of);
+                                (TENSOR == 0 ? a.rotate_k : a.rotate_v) != 0, a.clip, slot_of, lane);
 }
 
 template <int G, int BITS>

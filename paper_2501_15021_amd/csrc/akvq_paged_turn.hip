@@ -2,8 +2,12 @@
 // values are rotated, quantized and packed (akvq_pageblock.h), to 2 or 4 bits a code.
 //
 // A workgroup takes 32 rows of a sequence that share a block of the cache, and some of their heads.  The angles of these rows, 64 bits each, are
-// formed once for all heads and lie in LDS; then its four wavefronts take a head each: of the queries (turned: 16 bytes a lane, both sides of eight
+// formed once for all heads and lie in LDS; then its eight wavefronts take a head each: of the queries (turned: 16 bytes a lane, both sides of eight
 // pairs), of the keys (turned in the layout of the transform, written out and quantized) or of the values (quantized).
+//   Queries and keys out are written with the non-temporal hint: 8 x 4096 rows of 32 heads 302 us, 4.9 TB/s (a large copy: 5.47; plain stores 313,
+// with four wavefronts a workgroup 324), and attention after it takes as long.  Chunks of 500 to 1000 rows, 13 sequences of 28 / 4 heads, 45 us: a
+// round of workgroups, each a chain of lengths, positions, angles and two heads a wavefront; the next head asked for ahead (151 registers in place of
+// 120) takes as long.
 #include "akvq_device.h"
 #include "akvq_kernels.h"
 #include "akvq_pageblock.h"
@@ -12,6 +16,7 @@
 namespace akvq {
 namespace {
 
+constexpr int kTurnWaves = 8;
 constexpr int kTurnStride = 68;  // of a row's cosines in LDS: sixteen rows' 16-byte pieces fall on all banks
 
 // The rows that a call turns, and where they go: rows first .. first + rows - 1 of the chunk are rows base, base + 1, ... of the sequence; those
@@ -26,9 +31,9 @@ __device__ __forceinline__ TurnSpan turn_span(const PagedArgs &c, int b) {
 }
 
 template <int G, int BITS, bool INTERLEAVED>
-__global__ __launch_bounds__(256) void paged_turn_kernel(PagedTurnArgs a, int heads_per_group) {
+__global__ __launch_bounds__(64 * kTurnWaves, 4) void paged_turn_kernel(PagedTurnArgs a, int heads_per_group) {
   __shared__ __attribute__((aligned(16))) float cos_lds[kTokBlock][kTurnStride], sin_lds[kTokBlock][kTurnStride];
-  __shared__ int slot_of_lds[4][kTokBlock];
+  __shared__ int slot_of_lds[kTurnWaves][kTokBlock];
   const PagedArgs &c = a.append.c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int b = blockIdx.y, Hkv = c.Hkv, turned_heads = Hkv + a.Hq, heads = turned_heads + Hkv;  // keys, queries, values
@@ -41,7 +46,7 @@ __global__ __launch_bounds__(256) void paged_turn_kernel(PagedTurnArgs a, int he
   const bool stored = page >= 0 && page < c.n_pages;
   const int dim = a.plan.dim;
   if (first_head < turned_heads) {  // uniform
-    for (int r = wave; r < kTokBlock; r += 4)
+    for (int r = wave; r < kTokBlock; r += kTurnWaves)
       if (t0 + r >= s.base && t0 + r < t_turned && lane < dim / 2) {
         const Turn t = pair_turn(a.plan, lane, s.first + (t0 + r - s.base));
         cos_lds[r][lane] = t.c;
@@ -52,122 +57,132 @@ __global__ __launch_bounds__(256) void paged_turn_kernel(PagedTurnArgs a, int he
   // the chunk's row that is row t of the sequence; rows outside of the chunk read a clamped (valid) one, and nothing derived from it is stored
   auto chunk_row = [&](int t) { return (long long)s.first + min(max(t - s.base, 0), s.rows - 1); };
   auto turns_row = [&](int t) { return t >= s.base && t < t_turned; };
-  const int r = lane >> 2, j = lane & 3;
-
-  for (int job = first_head + wave; job < end_head; job += 4) {
-    if (job >= Hkv && job < turned_heads) {  // a query head: eight rows at a time
-      const int head = job - Hkv, o = lane & 7, turning = dim / 16;
-      const bool turns = o < turning;
-      const int at0 = INTERLEAVED ? 16 * o : turns ? 8 * o : dim + 16 * (o - turning), at1 = at0 + (!INTERLEAVED && turns ? dim / 2 : 8);
-      u32x4 x[4], y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint16_t *src = a.q + chunk_row(t0 + 8 * i + (lane >> 3)) * a.q_stride + head * kD;
-        x[i] = *reinterpret_cast<const u32x4 *>(src + at0);
-        y[i] = *reinterpret_cast<const u32x4 *>(src + at1);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = 8 * i + (lane >> 3);
-        if (turns) {
-          float cs[8], sn[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) { cs[e] = cos_lds[row][8 * o + e]; sn[e] = sin_lds[row][8 * o + e]; }
-          turn_chunks<INTERLEAVED>(x[i], y[i], cs, sn);
-        }
-        if (turns_row(t0 + row)) {
-          uint16_t *dst = a.q_out + chunk_row(t0 + row) * a.q_out_stride + head * kD;
-          *reinterpret_cast<u32x4 *>(dst + at0) = x[i];
-          *reinterpret_cast<u32x4 *>(dst + at1) = y[i];
-        }
-      }
-      continue;
-    }
-    const bool value = job >= turned_heads;
-    if (value && !stored) continue;
-    const int head = value ? job - turned_heads : job;
-    bool valid[2];
-    u32x4 raw[2][4];
+  const bool partial = t0 < s.base || t0 + kTokBlock > s.end;
+  auto pool_row = [&](int head) { return (((size_t)max(page, 0) * Hkv + head) << c.page_shift) + (t0 & ((1 << c.page_shift) - 1)); };
+  // Sines, cosines and addresses are made again for every head: kept for all of them they take 100 registers, and two wavefronts a SIMD are left.
+  auto again = [&] {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    return l;
+  };
+  auto load_rows = [&](const uint16_t *from, long long stride, int l, u32x4 (&raw)[2][4], bool (&valid)[2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int t = t0 + 16 * h + r;
+      const int t = t0 + 16 * h + (l >> 2);
       valid[h] = t >= s.base && t < s.end;
-      const uint16_t *row = (value ? a.append.v + chunk_row(t) * a.append.v_stride : a.append.k + chunk_row(t) * a.append.k_stride) + head * kD;
+      const uint16_t *row = from + chunk_row(t) * stride + 8 * (l & 3);
 #pragma unroll
-      for (int m = 0; m < 4; ++m) raw[h][m] = *reinterpret_cast<const u32x4 *>(row + 32 * m + 8 * j);
+      for (int m = 0; m < 4; ++m) raw[h][m] = *reinterpret_cast<const u32x4 *>(row + 32 * m);
     }
-    const size_t unit = (size_t)b * Hkv + head;
-    const size_t row0 = (((size_t)max(page, 0) * Hkv + head) << c.page_shift) + (t0 & ((1 << c.page_shift) - 1));
-    const bool partial = t0 < s.base || t0 + kTokBlock > s.end;
-    if (value) {
-      append_block<G, BITS, 1>(c, unit, t0, row0, raw, valid, partial, a.append.rotate_v != 0, a.append.clip, slot_of_lds[wave]);
-      continue;
-    }
-    if (!INTERLEAVED && dim < kD) {  // the other side of a chunk's pairs may be another lane's: read again
-      const int half = dim / 16;  // in chunks
+  };
+
+  auto write = [&](u32x4 *to, const u32x4 &x) {
+    __builtin_nontemporal_store(x, to);
+  };
+
+  int job = first_head + wave;
+  for (; job < min(end_head, Hkv); job += kTurnWaves) {  // a key head
+    const int l = again(), r = l >> 2, j = l & 3;
+    const uint16_t *from = a.append.k + job * kD;
+    bool valid[2];
+    u32x4 raw[2][4];
+    load_rows(from, a.append.k_stride, l, raw, valid);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint16_t *row = a.append.k + chunk_row(t0 + 16 * h + r) * a.append.k_stride + head * kD;
+    for (int h = 0; h < 2; ++h) {
+      const int row = 16 * h + r;
+      if (!INTERLEAVED && dim < kD) {  // the other side of a chunk's pairs may be another lane's: read again
+        const int half = dim / 16;  // in chunks
+        const uint16_t *at = from + chunk_row(t0 + row) * a.append.k_stride;
         u32x4 other[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
           const int chunk = 4 * m + j;
-          other[m] = *reinterpret_cast<const u32x4 *>(row + 8 * (chunk < half ? chunk + half : chunk < 2 * half ? chunk - half : chunk));
+          other[m] = *reinterpret_cast<const u32x4 *>(at + 8 * (chunk < half ? chunk + half : chunk < 2 * half ? chunk - half : chunk));
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
           const int chunk = 4 * m + j, pair = 8 * (chunk < half ? chunk : chunk - half);
           if (chunk < 2 * half) {
             const uint32_t flip = chunk < half ? 0x80000000u : 0u;  // (x, y) -> x c - y s; y c + x s
-            u32x4 y;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
               float v[2];
               const uint32_t ow = raw[h][m][w], pw = other[m][w];
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                const float cs = cos_lds[16 * h + r][pair + 2 * w + e], sn = __uint_as_float(__float_as_uint(sin_lds[16 * h + r][pair + 2 * w + e]) ^ flip);
+                const float cs = cos_lds[row][pair + 2 * w + e], sn = __uint_as_float(__float_as_uint(sin_lds[row][pair + 2 * w + e]) ^ flip);
                 const float own = half_bits_to_float(e ? ow >> 16 : ow & 0xFFFFu), oth = half_bits_to_float(e ? pw >> 16 : pw & 0xFFFFu);
                 v[e] = __fmaf_rn(own, cs, __fmul_rn(oth, sn));
               }
-              y[w] = turned_pair(v[0], v[1]);
+              raw[h][m][w] = turned_pair(v[0], v[1]);
             }
-            raw[h][m] = y;
           }
+        }
+      } else if (INTERLEAVED) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const int pair = 4 * (4 * m + j);
+          if (2 * pair < dim) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              float v0, v1;
+              const uint32_t x = raw[h][m][w];
+              turn_word(x, cos_lds[row][pair + w], sin_lds[row][pair + w], v0, v1);
+              raw[h][m][w] = turned_pair(v0, v1);
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          float cs[8], sn[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { cs[e] = cos_lds[row][32 * m + 8 * j + e]; sn[e] = sin_lds[row][32 * m + 8 * j + e]; }
+          turn_chunks<false>(raw[h][m], raw[h][m + 2], cs, sn);
         }
       }
-    } else {
+      if (turns_row(t0 + row)) {
+        uint16_t *dst = a.k_out + chunk_row(t0 + row) * a.k_out_stride + job * kD + 8 * j;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int m = 0; m < 4; ++m) write(reinterpret_cast<u32x4 *>(dst + 32 * m), raw[h][m]);
+      }
+    }
+    if (stored) append_block<G, BITS, 0>(c, (size_t)b * Hkv + job, t0, pool_row(job), raw, valid, partial, true, a.append.clip, slot_of_lds[wave], l);
+  }
+  for (; job < min(end_head, turned_heads); job += kTurnWaves) {  // a query head: eight rows at a time
+    const int l = again(), head = job - Hkv, o = l & 7, turning = dim / 16;
+    const bool turns = o < turning;
+    const int at0 = INTERLEAVED ? 16 * o : turns ? 8 * o : dim + 16 * (o - turning), at1 = at0 + (!INTERLEAVED && turns ? dim / 2 : 8);
+    u32x4 x[4], y[4];
 #pragma unroll
-        for (int m = 0; m < (INTERLEAVED ? 4 : 2); ++m) {
-          float cs[8], sn[8];
-          if (INTERLEAVED) {
-            const int pair = 4 * (4 * m + j);
-            if (2 * pair < dim) {
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                float v0, v1;
-                const uint32_t x = raw[h][m][w];
-                turn_word(x, cos_lds[16 * h + r][pair + w], sin_lds[16 * h + r][pair + w], v0, v1);
-                raw[h][m][w] = turned_pair(v0, v1);
-              }
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { cs[e] = cos_lds[16 * h + r][32 * m + 8 * j + e]; sn[e] = sin_lds[16 * h + r][32 * m + 8 * j + e]; }
-            turn_chunks<false>(raw[h][m], raw[h][m + 2], cs, sn);
-          }
-        }
+    for (int i = 0; i < 4; ++i) {
+      const uint16_t *src = a.q + chunk_row(t0 + 8 * i + (l >> 3)) * a.q_stride + head * kD;
+      x[i] = *reinterpret_cast<const u32x4 *>(src + at0);
+      y[i] = *reinterpret_cast<const u32x4 *>(src + at1);
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (turns_row(t0 + 16 * h + r)) {
-        uint16_t *dst = a.k_out + chunk_row(t0 + 16 * h + r) * a.k_out_stride + head * kD;
+    for (int i = 0; i < 4; ++i) {
+      const int row = 8 * i + (l >> 3);
+      if (turns) {
+        float cs[8], sn[8];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) *reinterpret_cast<u32x4 *>(dst + 32 * m + 8 * j) = raw[h][m];
+        for (int e = 0; e < 8; ++e) { cs[e] = cos_lds[row][8 * o + e]; sn[e] = sin_lds[row][8 * o + e]; }
+        turn_chunks<INTERLEAVED>(x[i], y[i], cs, sn);
       }
-    if (stored) append_block<G, BITS, 0>(c, unit, t0, row0, raw, valid, partial, true, a.append.clip, slot_of_lds[wave]);
+      if (turns_row(t0 + row)) {
+        uint16_t *dst = a.q_out + chunk_row(t0 + row) * a.q_out_stride + head * kD;
+        write(reinterpret_cast<u32x4 *>(dst + at0), x[i]);
+        write(reinterpret_cast<u32x4 *>(dst + at1), y[i]);
+      }
+    }
+  }
+  if (!stored) return;
+  for (; job < end_head; job += kTurnWaves) {  // a value head
+    const int l = again(), head = job - turned_heads;
+    bool valid[2];
+    u32x4 raw[2][4];
+    load_rows(a.append.v + head * kD, a.append.v_stride, l, raw, valid);
+    append_block<G, BITS, 1>(c, (size_t)b * Hkv + head, t0, pool_row(head), raw, valid, partial, a.append.rotate_v != 0, a.append.clip, slot_of_lds[wave], l);
   }
 }
 
@@ -243,8 +258,12 @@ void launch_variant(const PagedTurnArgs &a, hipStream_t stream) {
     return;
   }
   const int blocks = (c.max_rows + 30) / kTokBlock + 1;  // that max_rows rows can touch, wherever they start
-  const int per = 16;
-  const dim3 grid(blocks, c.B, (unsigned)((heads + per - 1) / per)), block(256);
+  // Heads of a workgroup, whose angles serve them all: two a wavefront, or one where that leaves the chip room.  Measured, us, 8 and 16 heads: 16 x 16
+  // rows of 96 heads in all (192 workgroups of 16) 12.6 and 13.6, 4 x 1024 (792) 42.7 and 47.3, 8 x 4096 (6192) 356 and 302; 2 x 1024 of 48
+  // (198) 13.2 and 13.9; of 36 heads 512 (51) 9.0 and 10.1, 32 x 8 (192) 9.2 and 8.5, 8 x 700 (552) 22.5 and 21.6, 13 of up to 1024 45.7 and 45.4.
+  const long long groups = (long long)blocks * c.B * ((heads + 15) / 16);
+  const int per = groups < (heads >= 48 ? 1024 : 64) ? 8 : 16;
+  const dim3 grid(blocks, c.B, (unsigned)((heads + per - 1) / per)), block(64 * kTurnWaves);
   if (a.plan.interleaved) paged_turn_kernel<G, BITS, true><<<grid, block, 0, stream>>>(a, per);
   else paged_turn_kernel<G, BITS, false><<<grid, block, 0, stream>>>(a, per);
 }
