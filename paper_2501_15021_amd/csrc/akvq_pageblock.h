@@ -24,6 +24,19 @@ __device__ __forceinline__ uint32_t code_bits_of(float u, const GroupQ &g) {
 }
 constexpr uint32_t kPack8Bias = (uint32_t)(0x4B400000ull * 0x11111111ull);  // sum over s < 8 of kMagicBits << 4s
 
+// Eight words, each or-ed over the four lanes that lie 4 apart in a row of 16.  Assembly, because the compiler spends a move on every other one of these.
+// (The leading s_nop covers the wait states of a DPP read after a VALU write of its source and after an EXEC write; inside, seven
+// instructions lie between a write and its read.)
+__device__ __forceinline__ void or_over_rows(uint32_t (&x)[8]) {
+#define AKVQ_OR8(CTRL)                                                                                                     \
+  "v_or_b32_dpp %0, %0, %0 " CTRL "\n\tv_or_b32_dpp %1, %1, %1 " CTRL "\n\tv_or_b32_dpp %2, %2, %2 " CTRL                 \
+  "\n\tv_or_b32_dpp %3, %3, %3 " CTRL "\n\tv_or_b32_dpp %4, %4, %4 " CTRL "\n\tv_or_b32_dpp %5, %5, %5 " CTRL             \
+  "\n\tv_or_b32_dpp %6, %6, %6 " CTRL "\n\tv_or_b32_dpp %7, %7, %7 " CTRL "\n\t"
+  asm volatile("s_nop 4\n\t" AKVQ_OR8("row_ror:4 row_mask:0xf bank_mask:0xf") AKVQ_OR8("row_ror:8 row_mask:0xf bank_mask:0xf")
+               : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
+#undef AKVQ_OR8
+}
+
 // slot_of[r] = rank in the ascending list of the block's row t0 + r, or -1.  The block's entries are one run of at most 32: the list is
 // sampled until the run starts within 64 entries of a sample, and two loads cover it.
 __device__ __forceinline__ void block_slots(const int32_t *sidx, int cnt, int t0, int lane, int *slot_of) {
@@ -174,14 +187,11 @@ __device__ __forceinline__ void append_block(const PagedArgs &c, size_t unit, in
     const uint32_t shifted_bias = 0u - ((BITS == 2 ? kPack4Bias : kMagicBits) << (BITS * ii));
     uint32_t w[BITS][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int mp = 0; mp < BITS; ++mp) {
 #pragma unroll
-      for (int mp = 0; mp < BITS; ++mp) {
-        uint32_t x = (vcode[mp][i] << (BITS * ii)) + shifted_bias;
-        x |= dpp_move_u<kRowRor4>(x);
-        x |= dpp_move_u<kRowRor8>(x);
-        w[mp][i] = x;
-      }
+      for (int i = 0; i < 8; ++i) w[mp][i] = (vcode[mp][i] << (BITS * ii)) + shifted_bias;
+      or_over_rows(w[mp]);
+    }
     if (mask == 0u) return;  // no new row in this lane's chunk
     // each of the four rows stores two of the eight chunks: i = 2*ii and 2*ii + 1 (pinned to registers: an indexed array would be
     // moved to LDS)
