@@ -387,9 +387,9 @@ int akvq_paged_attention(const akvq_paged *c, const akvq_chunk *rows, const void
  *     k_codes, v_codes [n_pages][Hkv][page_rows/32][512 words]; meta words, 16-bit rows, lists, table and lengths as above.
  *       keys, row r of its block, channel e: m=e/32, j=(e%32)/8, i=e%8: word = r/16*256 + (16*j + r%16)*4 + m;  bits [4i, 4i+4).
  *       values: half=r/16, q=(r%16)/4, ii=r%4, nb=e/16, n=e%16: word = nb%2*256 + (16*q + n)*4 + nb/2;  bits [16*half + 4*ii, +4).
- *   akvq_paged_nibble_bytes, akvq_paged_nibble_append, akvq_paged_nibble_default_splits, akvq_paged_nibble_attention: as the calls without "nibble", their arguments,
- *   refusals and what they promise of rows, pages, lengths and lists among it, over such pools; workspaces are sized by
- *   akvq_paged_workspace_bytes.  A cache that one kind of call has written means nothing to the other kind.
+ *   akvq_paged_nibble_bytes, akvq_paged_nibble_append, akvq_paged_nibble_default_splits, akvq_paged_nibble_attention: as the calls
+ *   without "nibble", their arguments, refusals and what they promise of rows, pages, lengths and lists among it, over such pools;
+ *   workspaces are sized by akvq_paged_workspace_bytes.  A cache that one kind of call has written means nothing to the other kind.
  *   Scores of cached rows: the query as an integer of 20 bits, codes as they are.  Weights have 11 bits, cached values as with 2 bits.
  */
 int akvq_paged_nibble_bytes(const akvq_paged *shape, size_t out_bytes[8]);

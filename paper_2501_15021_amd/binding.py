@@ -582,8 +582,8 @@ _PLAIN_PAGED = PagedCache.paged_struct  # as _PLAIN
 
 def paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int, clip: float,
                  flags: int = 0) -> None:
-    """akvq_paged_append (akvq_paged_nibble_append for a cache of 4-bit codes): rows k, v [n, Hkv, 128] fp16 of a chunk, row_start[b] to row_start[b + 1] those of sequence b (max_rows at
-    most), become its cache rows from seq_len[b] on.  cache.seq_len is the caller's to advance."""
+    """akvq_paged_append (akvq_paged_nibble_append for a cache of 4-bit codes): rows k, v [n, Hkv, 128] fp16 of a chunk, row_start[b] to
+    row_start[b + 1] those of sequence b (max_rows at most), become its cache rows from seq_len[b] on.  cache.seq_len is the caller's to advance."""
     st = (_native or native()).paged_append(cache, k, v, row_start, max_rows, clip, flags)
     if st:
         _check(st, "akvq_paged_append")
@@ -605,9 +605,9 @@ def paged_append_rotary(cache: PagedCache, rotary: Rotary, pos: torch.Tensor, q:
 def paged_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int,
                     sm_scale: float, n_split: int = 0, flags: int = 0, out: Optional[torch.Tensor] = None,
                     lse: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """akvq_paged_attention (akvq_paged_nibble_attention for a cache of 4-bit codes): a chunk's rows q [n, Hq, 128], k and v [n, Hkv, 128] fp16 (row_start and max_rows as in paged_append) over the
-    cached rows of their sequences and over the chunk's own rows up to each.  Returns out [n, Hq, 128] fp16; lse [n, Hq] fp32 is
-    written where given.  Rows that belong to no sequence, or lie behind max_rows of one, are left as they are: without out= they hold
+    """akvq_paged_attention (akvq_paged_nibble_attention for a cache of 4-bit codes): a chunk's rows q [n, Hq, 128], k and v [n, Hkv, 128] fp16
+    (row_start and max_rows as in paged_append) over the cached rows of their sequences and over the chunk's own rows up to each.  Returns
+    out [n, Hq, 128] fp16; lse [n, Hq] fp32 is written where given.  Rows that belong to no sequence, or lie behind max_rows of one, are left as they are: without out= they hold
     whatever was there.  out may not overlap q, k or v.  The workspace is of its own for every call: calls on two
     streams, or two captured graphs, share none."""
     st, out = (_native or native()).paged_attention(cache, q, k, v, row_start, max_rows, sm_scale, n_split, flags, out, lse)

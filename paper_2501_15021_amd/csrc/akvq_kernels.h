@@ -486,7 +486,7 @@ inline int paged_splits(long units, long tokens, long R, long len, PagedKind kin
   return (int)paged_tile_splits(paged_tile_rows(units, tokens, R, len, kind), units, tokens, R, len, kind);
 }
 
-// ---- pages of 4-bit codes: the same calls over pools of twice the words (akvq_paged4.hip, akvq_paged4_attention.hip) ----
+// ---- pages of 4-bit codes: the same calls over pools of twice the words (akvq_paged_append.hip, akvq_paged4_attention.hip) ----
 hipError_t launch_paged4_append(const PagedAppendArgs &a, int G, hipStream_t stream);
 hipError_t launch_paged4_attention(const PagedAttentionArgs &a, int G, hipStream_t stream);
 

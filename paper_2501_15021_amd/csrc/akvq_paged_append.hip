@@ -5,6 +5,8 @@
 // and a block that is only partly new has one writer.  Memory and instruction issue bound it alike (512 bytes in, 72 or 80 out and 11
 // operations an element): sixteen prompts of 4096 rows, 32 heads, 251 us, 4.9 TB/s (a large copy: 5.47).  Chunks of 500 to 1000 rows, 13
 // sequences of 4 heads, a seventh of the rows 16-bit, 13 us: a round of wavefronts, latency (the list's samples 2 us of it, the overlay 1).
+//   4 bits a code (twice the words, the same loads and rotation; 13 operations an element): 12 prompts of up to 4095 rows, 32 heads, 149 us,
+// 4.7 TB/s, the vector unit 77 % busy; one row of each of 16 sequences as with 2 bits.
 #include "../../include/akvq.h"
 #include "akvq_device.h"
 #include "akvq_kernels.h"
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(64) void paged_append_row_kernel(PagedAppendArgs a)
   append_row_wave<G, SampledSlot>(q, unit, blockIdx.y, threadIdx.x, code_lds, row_lds);
 }
 
-// The same into pages of 4-bit codes
+// The same into pages of 4-bit codes: the row's words are joined with their neighbours' nibbles, which for values lie in words of four rows.
 template <int G>
 __global__ __launch_bounds__(64) void paged4_append_row_kernel(PagedAppendArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t code_lds[kD];

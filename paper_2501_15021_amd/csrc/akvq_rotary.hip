@@ -6,6 +6,8 @@
 // for all heads (64 bits, 50 instructions) and leaves its sine and cosine in LDS, from where lane (h, o) takes those of pairs 8o .. 8o + 7 for
 // every eighth head.  A lane owns two chunks of eight channels, which hold both sides of its eight pairs in either layout (half: chunks that
 // lie dim / 2 apart; interleaved: neighbours), or two chunks that do not turn: so a row may be turned in place.
+//   8 x 8191 rows of 28 / 4 heads, 64 of 128 channels turning: 137 us, 5.2 TB/s (a large copy: 5.47; written with the non-temporal hint 161).
+// 16 rows of 64 heads: 2.65 us, a chain of one load, the angle and one store.
 #include "akvq_device.h"
 #include "akvq_kernels.h"
 #include "akvq_turn.h"
