@@ -490,7 +490,13 @@ struct Pages {
     if (!k.p) throw Failed();
     here(tensor(k.p));
     if (held.p) return;
-    need(bits == 2 || tensor(k.p).numel() == (int64_t)c.n_pages * c.Hkv * c.page_rows * 16, "k_codes is no pool of 4-bit codes");
+    if (bits == 4) {  // (a pool of 2-bit codes has half the words)
+      Held v(PyObject_GetAttr(cache, names.v_codes));
+      if (!v.p) throw Failed();
+      const int64_t words = (int64_t)c.n_pages * c.Hkv * c.page_rows * 16;
+      need(tensor(k.p).numel() == words, "k_codes is no pool of 4-bit codes");
+      need(tensor(v.p).numel() == words, "v_codes is no pool of 4-bit codes");
+    }
     Held t(PyObject_GetAttr(cache, names.table)), s(PyObject_GetAttr(cache, names.seq_len));
     if (!t.p || !s.p) throw Failed();
     const at::Tensor &table = tensor(t.p), &len = tensor(s.p);

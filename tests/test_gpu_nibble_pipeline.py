@@ -235,6 +235,16 @@ def test_pools_of_another_kind_are_refused():
         akvq.paged_attention(s.cache, s.q, s.k, s.v, s.row_start, 2, SM)
 
 
+def test_pools_of_two_kinds_are_refused():
+    s = sequences([10], [2], HKV, 128, Hq=HQ)
+    s.cache.v_codes = Sequences([10], [2], HKV, 128, Hq=HQ).cache.v_codes
+    pos = torch.zeros(3, 2, dtype=torch.int32, device="cuda")
+    with pytest.raises(akvq.AkvqError, match="v_codes is no pool of 4-bit codes"):
+        akvq.paged_append_rotary(s.cache, PLANS["half"], pos, s.q, s.k, s.v, s.row_start, 2, CLIP)
+    with pytest.raises(akvq.AkvqError, match="v_codes is no pool of 4-bit codes"):
+        akvq.paged_attention(s.cache, s.q, s.k, s.v, s.row_start, 2, SM)
+
+
 def test_a_cache_that_describes_itself():
     """... is asked, and says how many bits a code has."""
     class Own(akvq.PagedCache):
