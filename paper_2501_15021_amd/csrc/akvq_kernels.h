@@ -435,6 +435,10 @@ constexpr int kPagedManyRows = 256;  // of a workgroup that has many; its number
 // Codes of 4 bits: with one group a row three workgroups of 16 rows run on a CU, and rounds of them even out what memory gives each: one row
 // over 16384 rows of 512 units, 512 workgroups 219, 1536 190, 2048 188; of 256 units over up to 16384, 768 81.5, 1536 78.6; with two groups two
 // run: over 32768 of 128 units, 512 116, 768 128, 1024 122, over up to 16384, 58, 70 and 63.
+// A wavefront takes two blocks at a time for about 1 us, the merge costs 2 us and reads sixteen splits at a time, for 0.8 more a time.  One row over 320
+// rows of 32 units, 1 and 2 splits 8.9 and 9.8, over 432 9.2 and 9.8 (3 splits), over 480 10.3 and 9.7 (4 splits of 8 units); 16 rows over 432
+// 9.6 and 10.7, over 480 10.9 and 10.8; one row over 3000 of 8 units, 12 splits 9.7, 16 9.8, 23 10.6; over 3600 16 9.7, 28 10.5 (a
+// seventh of the rows 16-bit: over 3000 12.0, 10.3 and 11.0, over 3300 12.0, 12.0 and 10.9).
 struct PagedKind { int bits = 2, G = 128; };
 inline long paged_tile_splits(long per, long units, long tokens, long R, long len, PagedKind kind = {}) {
   const long blocks = (len + tokens + 31) / 32, tiles = (tokens * R + per - 1) / per;
@@ -445,7 +449,10 @@ inline long paged_tile_splits(long per, long units, long tokens, long R, long le
     if (n > want) want = n;
   };
   if (per == 16) {
-    fill(256, 4); fill(512, 8);
+    if (kind.bits == 4 && blocks <= 15) return 1;
+    fill(256, 4);
+    if (kind.bits == 4 && blocks <= 120 && want > 16) want = 16;
+    fill(512, 8);
     if (kind.bits == 2 || kind.G == 128) fill(768, 64);
     if (kind.bits == 4 && kind.G == 128) fill(2304, 85);
   }

@@ -21,3 +21,9 @@ def test_splits():
     """One token a sequence: the choices that the rule's comment measures."""
     assert [n for _, n, _, _ in tiles([(512, 1, 1, 16384, 128), (512, 1, 1, 4096, 128), (256, 1, 1, 16384, 128), (128, 1, 7, 32768, 64), (512, 1, 1, 8192, 64),
                                        (32, 1, 1, 640, 128)])] == [4, 1, 6, 4, 1, 5]
+
+
+def test_splits_of_short_calls():
+    """No merge where a wavefront has two pairs of blocks at most, and one reading of partial sums where sixteen splits leave it one."""
+    assert [n for _, n, _, _ in tiles([(32, 1, 1, 320, 128), (32, 1, 1, 479, 128), (32, 1, 1, 480, 128), (32, 16, 1, 432, 128), (8, 1, 1, 3000, 128),
+                                       (8, 1, 1, 3839, 128), (8, 1, 1, 3840, 128)])] == [1, 1, 4, 1, 16, 16, 30]
