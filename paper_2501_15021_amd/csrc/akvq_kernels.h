@@ -433,8 +433,9 @@ constexpr int kPagedManyRows = 256;  // of a workgroup that has many; its number
 // 32, 256 40.4, 512 37.0; of 256 units over 4096, 256 38.5, 512 42.7, over 8192 70 and 64; one row over 640 of 32 units, 2 splits 10.8, 5
 // splits 9.5.
 // Codes of 4 bits: with one group a row three workgroups of 16 rows run on a CU, and rounds of them even out what memory gives each: one row
-// over 16384 rows of 512 units, 512 workgroups 219, 1536 190, 2048 188; of 256 units over up to 16384, 768 81.5, 1536 78.6; with two groups two
-// run: over 32768 of 128 units, 512 116, 768 128, 1024 122, over up to 16384, 58, 70 and 63.
+// over 16384 rows of 512 units, 512 workgroups 219, 1536 190, 2048 188; of 256 units over up to 16384, 768 81.5, 1536 78.6; with two groups and up
+// to eight rows, over 32768 of 128 units, 512 116, 768 110, 1024 120, 1536 117, over up to 16384, 58, 55, 61 and 60, over 16384 of 512 units
+// 512 219, 1536 209, 2048 213; with more rows two run: 16 over 8192 of 256 units, 512 71, 768 82.
 // A wavefront takes two blocks at a time for about 1 us, the merge costs 2 us and reads sixteen splits at a time, for 0.8 more a time.  One row over 320
 // rows of 32 units, 1 and 2 splits 8.9 and 9.8, over 432 9.2 and 9.8 (3 splits), over 480 10.3 and 9.7 (4 splits of 8 units); 16 rows over 432
 // 9.6 and 10.7, over 480 10.9 and 10.8; one row over 3000 of 8 units, 12 splits 9.7, 16 9.8, 23 10.6; over 3600 16 9.7, 28 10.5 (a
@@ -453,8 +454,9 @@ inline long paged_tile_splits(long per, long units, long tokens, long R, long le
     fill(256, 4);
     if (kind.bits == 4 && blocks <= 120 && want > 16) want = 16;
     fill(512, 8);
-    if (kind.bits == 2 || kind.G == 128) fill(768, 64);
+    if (kind.bits == 2 || kind.G == 128 || tokens * R <= 8) fill(768, 64);
     if (kind.bits == 4 && kind.G == 128) fill(2304, 85);
+    else if (kind.bits == 4 && tokens * R <= 8) fill(1536, 170);
   }
   else if (per == 32) { fill(256, 8); fill(512, want == 1 ? 128 : 32); }
   else fill(256, 8);

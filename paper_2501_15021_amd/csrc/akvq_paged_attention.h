@@ -81,7 +81,7 @@ __device__ __forceinline__ Halves neighbours(float v) {
   return {__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
 // The value of lane l ^ 8.
-__device__ __forceinline__ float other_eight(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, false)); }  // row_ror:8
+__device__ __forceinline__ float other_eight(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xF, 0xF, true)); }  // row_ror:8
 __device__ __forceinline__ float halves_max(float v) {
   const Halves h = halves(v);
   return fmaxf(h.lo, h.hi);
@@ -428,8 +428,10 @@ struct PagedShared<G, 32, false, BITS> {
 };
 
 // EIGHT: no workgroup has more than eight rows (of a tile of 16): the two columns of each also share the digits of its query.
+//   Three workgroups of a tile of 16 run on a CU (168 registers), two of those with two groups of 4-bit codes and more than eight rows (16 rows
+// of 256 units over 8192: 71 us, three at a time and one block after the other 72).
 template <int G, int W, bool MANY, int BITS, bool EIGHT = false>
-__global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(BITS == 4 && G == 64) ? 3 : 2) void paged_attention_kernel(PagedAttentionArgs a) {
+__global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(BITS == 4 && G == 64 && !EIGHT) ? 3 : 2) void paged_attention_kernel(PagedAttentionArgs a) {
   static_assert(BITS == 2 || kDigits == 4);
   static_assert(!EIGHT || (W == 16 && BITS == 4));
   typedef Tile<W> T;
@@ -1175,19 +1177,21 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
           after = locate(blk + 4);
           if (!EIGHT || blk + 4 < code_end) ask_meta(after);
         }
+        // (EIGHT with two groups: one after the other, and codes asked for that may not be used, so that three workgroups run on a CU: one row over
+        // 32768 rows of 128 units 108-112 us, both at once and two workgroups 117-120; a call of one pair of blocks each 10.5 against 10.4)
         const BlockMeta<NG> (&bm)[2] = bms[turn];
-        if constexpr (kWide) {
+        if constexpr (kWide || (EIGHT && NG == 2)) {
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             if (x == 1 && blk + 1 >= code_end) break;
             float y[NY];
             scores(bm[x], y, codes_of(x));
-            if (more) few_k[x] = load_codes(c.k_codes, next.at[x]);
+            few_k[x] = load_codes(c.k_codes, next.at[x]);
             raise_codes(y);
             weights(bm[x], y);
             values(few_v[kOneValue ? 0 : x], bm[x], far, y);
             if constexpr (kOneValue) few_v[0] = load_codes(c.v_codes, x == 0 ? now.at[1] : next.at[0]);
-            else if (more) few_v[x] = load_codes(c.v_codes, next.at[x]);
+            else few_v[x] = load_codes(c.v_codes, next.at[x]);
           }
         } else {  // both at once: what one waits for the other covers
           float y0[NY], y1[NY];

@@ -20,7 +20,8 @@ def test_few_rows():
 def test_splits():
     """One token a sequence: the choices that the rule's comment measures."""
     assert [n for _, n, _, _ in tiles([(512, 1, 1, 16384, 128), (512, 1, 1, 4096, 128), (256, 1, 1, 16384, 128), (128, 1, 7, 32768, 64), (512, 1, 1, 8192, 64),
-                                       (32, 1, 1, 640, 128)])] == [4, 1, 6, 4, 1, 5]
+                                       (32, 1, 1, 640, 128),
+                                       (128, 1, 7, 16384, 64), (512, 1, 1, 16384, 64), (256, 2, 8, 8192, 64)])] == [4, 1, 6, 6, 1, 5, 6, 3, 2]
 
 
 def test_splits_of_short_calls():
