@@ -109,9 +109,9 @@ def cached_rows(s, b, t):
 
 def check_attention(s, got, lse, sm_scale, what=""):
     """Attention from its formula in 64 bits on what the pages hold.  Bounds, per row in the 2-norm (which the rotation keeps): a score is off by
-    2^-15 |q| |k| sm_scale (queries of 20 and 16 bits, and 32-bit sums), a weight by twice that and by half a step of binary16, 2^-11; with two
-    groups a row its product with a group's scale is rounded once more, 2^-11; and the result by its own rounding, 2^-11 of it (2^-25
-    an element where it is below the smallest normal number)."""
+    2^-15 |q| |k| sm_scale (queries of 20 and 16 bits, and 32-bit sums), a weight by twice that and by half a step of binary16, 2^-11 (with two
+    groups a row it is the product with a group's scale that is rounded); and the result by its own rounding, 2^-11 of it (2^-25 an element
+    where it is below the smallest normal number)."""
     for b in range(s.cache.B):
         lo, hi, t = s.starts[b], s.starts[b + 1], s.lens[b]
         n, R = hi - lo, s.Hq // s.Hkv
@@ -128,8 +128,7 @@ def check_attention(s, got, lse, sm_scale, what=""):
             want, wlse = p @ v, torch.logsumexp(logits, 1)
             score = 2.0 ** -15 * abs(sm_scale) * s.q[lo:hi, h].double().norm(dim=1) * (mask * k.norm(dim=1)).amax(1)
             err = (got[lo:hi, h].double() - want).norm(dim=1)
-            rounding = 2.0 ** -11 * (1 if s.G == 128 else 2)
-            bound = 2.0 ** -11 * want.norm(dim=1) + 2.0 ** -25 * 128 ** 0.5 + (rounding + 2 * score + 2.0 ** -18) * (p @ v.norm(dim=1))
+            bound = 2.0 ** -11 * want.norm(dim=1) + 2.0 ** -25 * 128 ** 0.5 + (2.0 ** -11 + 2 * score + 2.0 ** -18) * (p @ v.norm(dim=1))
             assert bool((err <= bound).all()), (what, b, h, float((err / bound).max()), float((err / want.norm(dim=1)).max()))
             if lse is not None:
                 d = (lse[lo:hi, h].double() - wlse).abs()
