@@ -34,9 +34,9 @@
 // Pages of 4-bit codes (BITS = 4) take the same way.  A key's nibbles, two masked words for eight of them, are the 8-bit floats code * 2^-9 as they
 // lie (subnormals among them), at twice the price of a 4-bit product; tiles of 256, which expand a block once for all, repack them as 6-bit floats
 // code / 8, at its price.  A value's nibbles are masked in place, two a byte: code * 16^(ii mod 2) * 2^-24.
-//   One row over 2048 to 4096 rows of 512 units 42-43 us, 3.9 TB/s, of which 10 to 12 lie before the first block and behind the last (in between
-// 6.2 TB/s); one of 4 heads over 32768 rows of 128 units (G = 64) 113 us, 5.4 TB/s; one over 640 rows of 32 units 8.0 and 2.9 for the merge.
-// 4 x 2048 rows of 32 heads over 8192 cached ones: 1.31 ms, 940 TFLOP/s, under the power limit as with 2 bits.
+//   One row over 2048 to 4096 rows of 512 units 42 us, 5.0 TB/s, of which 10 to 12 lie before the first block and behind the last (in between
+// 6.2 TB/s); one of 7 heads over 32768 rows of 128 units (G = 64) 110 us, 5.5 TB/s; one over 640 rows of 32 units 7.8 and 2.9 for the merge.
+// 4 x 2048 rows of 32 heads over 8192 cached ones: 1.31-1.35 ms, 920-945 TFLOP/s, under the power limit as with 2 bits.
 #pragma once
 #include "akvq_device.h"
 #include "akvq_kernels.h"
