@@ -410,6 +410,7 @@ struct PagedAppendArgs {
   long long k_stride, v_stride;
   float clip;
   int rotate_k, rotate_v;
+  int heads_first;  // workgroups of the same rows lie next to each other, not those of a head (set by the launcher)
 };
 hipError_t launch_paged_append(const PagedAppendArgs &a, int G, hipStream_t stream);
 
