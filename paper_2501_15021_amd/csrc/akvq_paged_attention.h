@@ -69,10 +69,9 @@ __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {  // round to 
   typedef __attribute__((ext_vector_type(2))) float f32x2;
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2));
 }
-// ... of a times the lower and b times the upper half of two binary16 numbers, one instruction each
-__device__ __forceinline__ uint32_t scaled_f16x2(float a, float b, uint32_t s) {
-  const f16x2 by = __builtin_bit_cast(f16x2, s);
-  const f16x2 x = {(_Float16)__builtin_fmaf(a, (float)by[0], 0.0f), (_Float16)__builtin_fmaf(b, (float)by[1], 0.0f)};
+// ... of a times s and b times t, one instruction each
+__device__ __forceinline__ uint32_t scaled_f16x2(float a, float b, float s, float t) {
+  const f16x2 x = {(_Float16)__builtin_fmaf(a, s, 0.0f), (_Float16)__builtin_fmaf(b, t, 0.0f)};
   return __builtin_bit_cast(uint32_t, x);
 }
 // The values of lanes l % 32 and l % 32 + 32, in every lane.
@@ -375,8 +374,8 @@ struct CodeBlock {
   __attribute__((aligned(16))) u32x4 v[2][4][kWave];
   // where some zero-point has one: minus its multiple of 1024, in the weights' order; of two groups of 2-bit codes times the share, in two binary16 terms
   __attribute__((aligned(16))) uint16_t v_far[NG][NG][32];
-  // of two groups of 4-bit codes: their scales times v_rcp, binary16 in the weights' order
-  __attribute__((aligned(16))) uint16_t v_share[BITS == 4 ? NG : 1][BITS == 4 && NG == 2 ? 32 : 1];
+  // of two groups of 4-bit codes: their scales times v_rcp (32 bits: a scale may be 2^-40 of the other, which no binary16 number holds)
+  __attribute__((aligned(16))) float v_share[BITS == 4 ? NG : 1][BITS == 4 && NG == 2 ? 32 : 1];
 };
 // The power of two at or below a positive number: its logarithm and reciprocal (of 0: -127 and 2^127).
 __device__ __forceinline__ float power_log(float x) { return (float)((int)(__float_as_uint(x) >> 23) - 127); }
@@ -1030,7 +1029,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
             to.v_rcp[r] = NG == 2 && row.part ? rcp : row.rcp;
             if constexpr (kGroupWeights)
 #pragma unroll
-              for (int g = 0; g < NG; ++g) to.v_share[g][weight_place(r)] = (uint16_t)float_to_half_bits_rne(row.scale[g] * rcp);
+              for (int g = 0; g < NG; ++g) to.v_share[g][r] = row.scale[g] * rcp;
           }
         } else {
           if constexpr (BITS == 2) {
@@ -1129,9 +1128,9 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), W == 16 && !(
 #pragma unroll
           for (int g = 0; g < NW; ++g) {
             if constexpr (kGroupWeights) {
-              const u32x4 s = *reinterpret_cast<const u32x4 *>(&bm.v_share[g][8 * (2 * st + g_lane)]);
+              const f32x4 s0 = *reinterpret_cast<const f32x4 *>(&bm.v_share[g][T::row(st, g_lane)]), s1 = *reinterpret_cast<const f32x4 *>(&bm.v_share[g][T::row(st + NA / 2, g_lane)]);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) w[g][st][i] = scaled_f16x2(y[4 * st + i], y[4 * st + NY / 2 + i], s[i]);
+              for (int i = 0; i < 4; ++i) w[g][st][i] = scaled_f16x2(y[4 * st + i], y[4 * st + NY / 2 + i], s0[i], s1[i]);
             } else {
 #pragma unroll
               for (int i = 0; i < 4; ++i) w[g][st][i] = pack_f16x2(y[4 * st + i], y[4 * st + NY / 2 + i]);
