@@ -458,7 +458,7 @@ def rope_axes(axes: RopeAxes, pos: torch.Tensor, q: Optional[torch.Tensor], k: O
               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False):
     """akvq_rope_axes: rotary positions of a chunk's rows, q [n, Hq, 128] and k [n, Hkv, 128] (either may be None), into q_out and k_out
     (new tensors where None; q and k themselves turn in place).  inverse: turns back, which is also the gradient; the call records none
-    itself and refuses rows that ask for one (a torch.autograd.Function calls it both ways).  Returns (q_out, k_out)."""
+    itself and refuses rows that ask for one or have a tangent (a torch.autograd.Function calls it both ways).  Returns (q_out, k_out)."""
     st, outs = (_native or native()).rope_axes(axes._struct, pos, q, k, q_out, k_out, inverse)
     if st:
         _check(st, "akvq_rope_axes")
@@ -517,7 +517,7 @@ def rotary_rows(rotary: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k:
                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False):
     """akvq_rotary_rows: rotary positions of a chunk's rows, as rope_axes, in either layout, of part of the head or all of it.  inverse: the
     transposed rotation, which is the gradient (with magnitude 1 it turns back); the call records none itself and refuses rows that ask
-    for one.  Returns (q_out, k_out)."""
+    for one or have a tangent.  Returns (q_out, k_out)."""
     st, outs = (_native or native()).rotary_rows(rotary._struct, pos, q, k, q_out, k_out, inverse)
     if st:
         _check(st, "akvq_rotary_rows")
@@ -595,7 +595,8 @@ def paged_append_rotary(cache: PagedCache, rotary: Rotary, pos: torch.Tensor, q:
     """akvq_paged_append_rotary: a chunk's queries (q may be None) and keys are turned as rotary_rows turns them, into q_out and k_out (new
     tensors where None; q and k themselves turn in place), and the turned keys and v become cache rows as paged_append writes them, in one
     call.  pos [axes, n] int32.  Rows that belong to no sequence, or lie behind max_rows of one, are left as they are, in q_out and k_out
-    too: new tensors hold whatever was there.  cache.seq_len is the caller's to advance.  Returns (q_out, k_out), for paged_attention."""
+    too: new tensors hold whatever was there.  cache.seq_len is the caller's to advance.  Queries and keys that ask for a gradient or have a
+    tangent are refused.  Returns (q_out, k_out), for paged_attention."""
     st, outs = (_native or native()).paged_append_rotary(cache, rotary._struct, pos, q, k, v, row_start, max_rows, clip, q_out, k_out, flags)
     if st:
         _check(st, "akvq_paged_append_rotary")

@@ -308,9 +308,10 @@ int64_t packed(const at::Tensor &t, const char *what, int64_t rows, int64_t head
 void written(const at::Tensor &t) {
   if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
-// No call here records a gradient.
+// No call here records a gradient, or carries a tangent (forward-mode derivatives; none is there where they are switched off, as in inference mode).
 void no_gradient(const at::Tensor &t, const char *what) {
   need(!t.requires_grad() || !c10::GradMode::is_enabled(), what, " asks for a gradient, which this call does not record (the inverse turns it back)");
+  need(!t._fw_grad(0).defined(), what, " has a tangent, which this call does not carry (it turns as the rows do)");
 }
 at::Tensor fresh(at::IntArrayRef shape, const at::Tensor &like) { return at::empty(shape, like.options().dtype(at::kHalf).requires_grad(false)); }
 
