@@ -610,7 +610,8 @@ def paged_attention(cache: PagedCache, q: torch.Tensor, k: torch.Tensor, v: torc
     (row_start and max_rows as in paged_append) over the cached rows of their sequences and over the chunk's own rows up to each.  Returns
     out [n, Hq, 128] fp16; lse [n, Hq] fp32 is written where given.  Rows that belong to no sequence, or lie behind max_rows of one, are left as they are: without out= they hold
     whatever was there.  out may not overlap q, k or v.  The workspace is of its own for every call: calls on two
-    streams, or two captured graphs, share none."""
+    streams, or two captured graphs, share none.  No gradient is recorded and no tangent carried: over 4-bit codes rows that ask for one or have one are
+    refused, over 2-bit codes the result comes without."""
     st, out = (_native or native()).paged_attention(cache, q, k, v, row_start, max_rows, sm_scale, n_split, flags, out, lse)
     if st:
         _check(st, "akvq_paged_attention")

@@ -309,9 +309,11 @@ void written(const at::Tensor &t) {
   if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 // No call here records a gradient, or carries a tangent (forward-mode derivatives; none is there where they are switched off, as in inference mode).
-void no_gradient(const at::Tensor &t, const char *what) {
-  need(!t.requires_grad() || !c10::GradMode::is_enabled(), what, " asks for a gradient, which this call does not record (the inverse turns it back)");
-  need(!t._fw_grad(0).defined(), what, " has a tangent, which this call does not carry (it turns as the rows do)");
+// gradient, tangent: what is said of them
+void no_gradient(const at::Tensor &t, const char *what, const char *gradient = " asks for a gradient, which this call does not record (the inverse turns it back)",
+                 const char *tangent = " has a tangent, which this call does not carry (it turns as the rows do)") {
+  need(!t.requires_grad() || !c10::GradMode::is_enabled(), what, gradient);
+  need(!t._fw_grad(0).defined(), what, tangent);
 }
 at::Tensor fresh(at::IntArrayRef shape, const at::Tensor &like) { return at::empty(shape, like.options().dtype(at::kHalf).requires_grad(false)); }
 
@@ -619,6 +621,12 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const float sm_scale = (float)number(a[6]);
     const long asked = integer(a[7]);
     const uint32_t flags = flags_of(a[8]);
+    if (pages.bits == 4) {  // (over 2-bit codes programs have been answered without a gradient, and still are)
+      static const char *const name[5] = {"q", "k", "v", "out", "lse"};
+      const at::Tensor *const t[5] = {&q, &k, &v, &out, &lse};
+      for (int i = 0; i < 5; ++i)
+        if (t[i]->defined()) no_gradient(*t[i], name[i], " asks for a gradient, which this call does not record (torch.no_grad answers without)", " has a tangent, which this call does not carry");
+    }
     Here here;
     for (const at::Tensor *t : {&q, &k, &v, &row_start, &out}) here(*t);
     if (lse.defined()) here(lse);
