@@ -464,8 +464,13 @@ inline long paged_tile_splits(long per, long units, long tokens, long R, long le
   return want < 64 ? want : 64;
 }
 // What a call takes in tiles of 32 or 256 rows, in us, by rounds of workgroups (two on a CU, or one): a beginning and end, and for every block
-// of 32 keys what was measured on full CUs.  Up to 11 % off the measurements below for tiles of 32 and 19 % for tiles of 256, the nearest pair 6 % apart
-// and 1 % in the estimate; it is there to compare the two, and is right in all nine.
+// of 32 keys what was measured on full CUs.  It is there to compare the two.  Codes of 2 bits: up to 11 % off the nine measurements below for tiles of 32
+// and 19 % for tiles of 256, the nearest pair 6 % apart and 1 % in the estimate, and right in all.  Codes of 4 bits, one group: up to 12 and 6 % off the
+// six below, right in all; four chunks of 2048 rows of 32 heads over 8192, which take 1330 us in tiles of 256 and 2030 in tiles of 32, it puts at 1659 and
+// 2228.  Two groups of 4-bit codes have no term of their own: measured times are 8 to 31 % above the estimate for tiles of 32 and 12 to 29 % for tiles of 256
+// (the long call 1640 and 2400 us, 1 % below and 8 % above), and it takes the quicker tile where their shares of the chip are alike.  It does not where one tile
+// of 256 more leaves them one split each: 8 units (R = 7) over 32768, 584 tokens take 751 us in 16 tiles and two splits, but 592 and 912 tokens get tiles of
+// 32 and one split, 1107 and 1535 us; in tiles of 256 and five splits they take 880 and 1248.
 inline double paged_tile_cost(long per, long units, long tokens, long R, long len, PagedKind kind = {}) {
   const long rows = tokens * R, tiles = (rows + per - 1) / per, splits = paged_tile_splits(per, units, tokens, R, len, kind);
   const double cached = len / 32.0, own = tokens / 32.0, merge = splits > 1 ? 5.0 : 0.0;
@@ -483,8 +488,9 @@ inline double paged_tile_cost(long per, long units, long tokens, long R, long le
 //     4 of 4096 over 64 71 and 59, 8 of 2048 42 and 48.
 // Codes of 4 bits, the same way: 28 rows of 32 units over 16384 (R = 7, G = 64) 36.0 in two tiles of 16 and 33.4 in one of 32, of 128 units 115 and
 // 91; 32 rows of 64 units over 8192 30.0 and 31.6; in tiles of 32 or 256, 256 units of 96 rows over 4096 100 and 121, of 200 221 and 165; 128 of 128
-// rows over 8192 110 and 125, of 256 214 and 191; 64 of 256 112 and 106; 4 of 585 tokens (R = 7, G = 64) over 2048 53 and 60; 8 of 1024 (R = 4)
-// over 32768 744 and 640.
+// rows over 8192 110 and 125, of 256 214 and 191; 64 of 256 112 and 106; 8 of 1024 (R = 4) over 32768 744 and 640.  With G = 64: 256 units of 96
+// rows over 4096 118 and 145, of 200 260 and 198; 128 of 128 rows over 8192 133 and 153, of 256 262 and 219; 64 of 256 131 and 124; 4 of 585 tokens
+// (R = 7) over 2048 52 and 62; 8 of 1024 (R = 4) over 32768 907 and 761, of 584 (R = 7) 896 and 751.
 inline long paged_tile_rows(long units, long tokens, long R, long len, PagedKind kind = {}) {
   const long rows = tokens * R;
   if (rows <= 16 || (rows <= 32 && units * ((len + 31) / 32) < 1L << (kind.bits == 4 && kind.G == 64 ? 14 : 15))) return 16;
