@@ -390,7 +390,9 @@ int akvq_paged_attention(const akvq_paged *c, const akvq_chunk *rows, const void
  *   akvq_paged_nibble_bytes, akvq_paged_nibble_append, akvq_paged_nibble_default_splits, akvq_paged_nibble_attention: as the calls
  *   without "nibble", their arguments, refusals and what they promise of rows, pages, lengths and lists among it, over such pools;
  *   workspaces are sized by akvq_paged_workspace_bytes.  A cache that one kind of call has written means nothing to the other kind.
- *   Scores of cached rows: the query as an integer of 20 bits, codes as they are.  Weights have 11 bits, cached values as with 2 bits.
+ *   Scores of cached rows: the query as an integer of 20 bits, codes as they are.  Weights have 11 bits (with G = 64 a set for each group of a row),
+ *   cached values are as they are.  Where the scales of a row's two groups lie far apart, a weight counts for the smaller one's channels down to
+ *   2^-27 of the row's largest weight times the ratio of the scales.
  */
 int akvq_paged_nibble_bytes(const akvq_paged *shape, size_t out_bytes[8]);
 int akvq_paged_nibble_append(const akvq_paged *c, const akvq_chunk *rows, const void *k, int64_t k_stride, const void *v,
@@ -407,7 +409,8 @@ int akvq_paged_nibble_attention(const akvq_paged *c, const akvq_chunk *rows, con
  *     c = magnitude * cos, s = magnitude * sin, each rounded once to 32 bits from an angle that is formed in 64;
  *     (x, y) -> (x c - y s, y c + x s): the second product is rounded to 32 bits, its sum with the first once, that to binary16.
  *   flags: AKVQ_ROPE_INVERSE (-s for s: the transposed rotation, which is the gradient; with magnitude 1 it turns the rows back) or 0.
- *   pos, q, k, q_out, k_out, strides, Hq, Hkv, n_rows: as in akvq_rope_axes.
+ *   pos, q, k, q_out, k_out, strides, Hq, Hkv, n_rows: as in akvq_rope_axes.  (That call forms sine and cosine another way: the same rows
+ *   turned by both differ by a unit in the last place of binary16 in less than 1 % of their elements.  akvq_paged_append_rotary has this call's bits.)
  */
 enum { AKVQ_ROTARY_HALF = 0, AKVQ_ROTARY_INTERLEAVED = 1 };
 typedef struct akvq_rotary {

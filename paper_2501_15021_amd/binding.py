@@ -515,7 +515,8 @@ class Rotary:
 
 def rotary_rows(rotary: Rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor] = None,
                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False):
-    """akvq_rotary_rows: rotary positions of a chunk's rows, as rope_axes, in either layout, of part of the head or all of it.  inverse: the
+    """akvq_rotary_rows: rotary positions of a chunk's rows, as rope_axes, in either layout, of part of the head or all of it (not rope_axes' bits:
+    less than 1 % of elements differ by a unit in the last place; paged_append_rotary's are the same).  inverse: the
     transposed rotation, which is the gradient (with magnitude 1 it turns back); the call records none itself and refuses rows that ask
     for one or have a tangent.  Returns (q_out, k_out)."""
     st, outs = (_native or native()).rotary_rows(rotary._struct, pos, q, k, q_out, k_out, inverse)

@@ -3,8 +3,9 @@
 //
 // One wavefront owns one 32-row block of one (sequence, kv-head, tensor), as there: pages hold whole blocks, so a block has one page,
 // and a block that is only partly new has one writer.  Memory and instruction issue bound it alike (512 bytes in, 72 or 80 out and 11
-// operations an element): sixteen prompts of 4096 rows, 32 heads, 251 us, 4.9 TB/s (a large copy: 5.47).  Chunks of 500 to 1000 rows, 13
-// sequences of 4 heads, a seventh of the rows 16-bit, 13 us: a round of wavefronts, latency (the list's samples 2 us of it, the overlay 1).
+// operations an element): sixteen prompts of 4096 rows, 32 heads, 251 us, 4.9 TB/s (a large copy: 5.47).  Chunks of 540 to 1024 rows of
+// 12 sequences, 4 heads, a seventh of the rows 16-bit, 14.7 us from memory and 11.4 where the last cache has the rows, without 16-bit ones 11.2 and
+// 9.3: a round of wavefronts, latency.
 //   4 bits a code (twice the words, the same loads and rotation; 13 operations an element): 12 prompts of up to 4095 rows, 32 heads, 149 us,
 // 4.7 TB/s, the vector unit 77 % busy; one row of each of 16 sequences as with 2 bits.
 #include "../../include/akvq.h"
@@ -118,7 +119,7 @@ template <int G, int BITS>
 hipError_t launch_blocks(PagedAppendArgs a, hipStream_t stream) {
   const int blocks = (a.c.max_rows + 30) / kTokBlock + 1, groups = (blocks + 3) / 4;  // blocks that max_rows rows can touch, wherever they start
   // Few workgroups: those of the same rows, whose heads lie next to each other in the chunk, run together.  Measured, us, that way and a head's together:
-  // 13 chunks of up to 1024 rows, 4 heads (936 workgroups) 10.2 and 10.6, 40 of 700 (1920) 15.7 and 16.3, 1 of 300, 32 heads (192) 4.5 and 4.8;
+  // 12 chunks of 540 to 1024 rows, 4 of 36 heads (936 workgroups in the grid, rows from memory) 11.1 and 11.4, with a seventh of them 16-bit 14.5 and 14.6, 40 of 700 (1920) 15.7 and 16.3, 1 of 300, 32 heads (192) 4.5 and 4.8;
   // 6 of 4000, 8 heads (3072) 25.6 and 25.2, 12 of up to 4095, 32 heads (25344) 140 and 137; 4 bits alike.
   a.heads_first = 2ll * groups * a.c.B * a.c.Hkv <= 2048 ? 1 : 0;
   const dim3 grid = a.heads_first ? dim3(groups * a.c.Hkv, a.c.B, 2) : dim3(groups, a.c.B * a.c.Hkv, 2);

@@ -35,8 +35,9 @@
 // lie (subnormals among them), at twice the price of a 4-bit product; tiles of 256, which expand a block once for all, repack them as 6-bit floats
 // code / 8, at its price.  A value's nibbles are masked in place, two a byte: code * 16^(ii mod 2) * 2^-24.
 //   One row over 2048 to 4096 rows of 512 units 42 us, 5.0 TB/s, of which 10 to 12 lie before the first block and behind the last (in between
-// 6.2 TB/s); one of 7 heads over 32768 rows of 128 units (G = 64) 110 us, 5.5 TB/s; one over 640 rows of 32 units 7.8 and 2.9 for the merge.
-// 4 x 2048 rows of 32 heads over 8192 cached ones: 1.31-1.35 ms, 920-945 TFLOP/s, under the power limit as with 2 bits.
+// 6.2 TB/s); one of 7 heads over 32768 rows of 128 units (G = 64) 110-115 us, 5.3-5.5 TB/s; one over 640 rows of 32 units 7.8 and 2.9 for the merge.
+// 4 x 2048 rows of 32 heads over 8192 cached ones: 1.30-1.44 ms, 860-950 TFLOP/s, 2.93 million cycles at 2.0 to 2.25 GHz (down to 1.8, a large
+// product's, where launches follow each other for long); with two groups 1.61-1.74 ms, 710-770 TFLOP/s, 3.74 million cycles.
 #pragma once
 #include "akvq_device.h"
 #include "akvq_kernels.h"
@@ -275,15 +276,15 @@ __device__ __forceinline__ u32x2 nibbles(uint32_t w) { return (u32x2){w & 0x0F0F
 template <int NG>
 struct BlockMeta {
   // Row operands of the product that a score starts with, sixteen bfloat16 slots.  First eight: minus the zero-point (low byte and multiples of
-  // 256, three times each: times the three terms of the query's sum), two terms of log2(V scale) / scale - 2 ii / scale (times 1).  Second
+  // 256, three times each: times the three terms of the query's sum), two terms of (log2(V scale) - code_place) / scale (times 1).  Second
   // eight: terms of 1 / scale (times those of minus the reference), the third term.  A row that takes no part has kNoScore for the
   // logarithm, a scale of 1 and nothing else.
   __attribute__((aligned(16))) uint16_t start[32][2][8];
   __attribute__((aligned(16))) uint16_t start2[NG == 2 ? 32 : 1][8];  // first eight of the second group's product: its zero-point
   __attribute__((aligned(16))) float k_scale[NG][32];
-  __attribute__((aligned(16))) float v_rcp[32];                       // 4^ii / V scale, the larger one where there are two (no part: 0)
+  __attribute__((aligned(16))) float v_rcp[32];                       // 2^code_place / V scale, the larger one where there are two (no part: 0)
   __attribute__((aligned(16))) float v_share[NG == 2 ? 2 : 1][32];    // V scale / the larger one
-  __attribute__((aligned(16))) uint16_t v_zero[2][NG][32];            // binary16, in the weights' order: zero-point * 4^(ii - 3), low part and multiples of 2048
+  __attribute__((aligned(16))) uint16_t v_zero[2][NG][32];            // binary16, in the weights' order: zero-point * 2^(code_place - 6), low part and multiples of 2048
 };
 
 template <int NG>

@@ -5,9 +5,10 @@
 // formed once for all heads and lie in LDS; then its eight wavefronts take a head each: of the queries (turned: 16 bytes a lane, both sides of eight
 // pairs), of the keys (turned in the layout of the transform, written out and quantized) or of the values (quantized).
 //   Queries and keys out are written with the non-temporal hint: 8 x 4096 rows of 32 heads 302 us, 4.9 TB/s (a large copy: 5.47; plain stores 313,
-// with four wavefronts a workgroup 324), and attention after it takes as long.  Chunks of 500 to 1000 rows, 13 sequences of 28 / 4 heads, 45 us: a
-// round of workgroups, each a chain of lengths, positions, angles and two heads a wavefront; the next head asked for ahead (151 registers in place of
-// 120) takes as long.
+// with four wavefronts a workgroup 324), and attention after it takes as long.  Chunks of 540 to 1024 rows of 12 sequences, 28 / 4 heads, a seventh of
+// the rows 16-bit, 2 bits: 46 us from memory, 36 where the last cache has the rows (without 16-bit rows 43 from memory).  888 workgroups with rows, of
+// which 512 run at a time, and every third has four heads for its eight wavefronts; each is a chain of lengths, positions, angles and two heads a
+// wavefront.  The next head asked for ahead (151 registers in place of 120) takes as long.
 #include "akvq_device.h"
 #include "akvq_kernels.h"
 #include "akvq_pageblock.h"
@@ -259,7 +260,7 @@ void launch_variant(const PagedTurnArgs &a, hipStream_t stream) {
   }
   const int blocks = (c.max_rows + 30) / kTokBlock + 1;  // that max_rows rows can touch, wherever they start
   // Heads of a workgroup, whose angles serve them all: two a wavefront, or one where that leaves the chip room.  Measured, us, 8 and 16 heads: 16 x 16
-  // rows of 96 heads in all (192 workgroups of 16) 12.6 and 13.6, 4 x 1024 (792) 42.7 and 47.3, 8 x 4096 (6192) 356 and 302; 2 x 1024 of 48
+  // rows of 96 heads in all (192 workgroups of 16 heads, in the grid) 12.6 and 13.6, 4 x 1024 (792) 42.7 and 47.3, 8 x 4096 (6192) 356 and 302; 2 x 1024 of 48
   // (198) 13.2 and 13.9; of 36 heads 512 (51) 9.0 and 10.1, 32 x 8 (192) 9.2 and 8.5, 8 x 700 (552) 22.5 and 21.6, 13 of up to 1024 45.7 and 45.4.
   const long long groups = (long long)blocks * c.B * ((heads + 15) / 16);
   const int per = groups < (heads >= 48 ? 1024 : 64) ? 8 : 16;
